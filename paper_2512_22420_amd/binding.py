@@ -14,6 +14,8 @@ LIB_PATH = os.path.join(HERE, "libnightjar.so")
 NJ_F32, NJ_BF16 = 0, 1
 NJ_OK, NJ_EINVAL, NJ_EDEVICE, NJ_EHIP, NJ_EAGAIN = 0, -1, -2, -3, -4
 NJ_DEV_BAD_TOKEN, NJ_DEV_BAD_BLOCK, NJ_DEV_BAD_CONTEXT, NJ_DEV_BAD_ACCEPT, NJ_DEV_SPLIT_WAIT = 1, 2, 4, 8, 16
+NJ_E4M3 = 2  # KV pages of nj_kv_layer only
+NJ_DEV_BAD_SAMPLING = 32
 NJ_GEMM_STORE, NJ_GEMM_RESIDUAL, NJ_GEMM_SWIGLU = 0, 1, 2
 NJ_GEMM_KBLOCKED = 16  # flag: x (and a SwiGLU y) k-blocked, [K/32][M][32]
 NJ_GEMM_AUTO, NJ_GEMM_STREAM, NJ_GEMM_TILE_256x256, NJ_GEMM_TILE_128x256, NJ_GEMM_TILE_128x128 = 0, 1, 2, 3, 4
@@ -43,6 +45,15 @@ class Weights(ctypes.Structure):
 
 class KvCache(ctypes.Structure):
     _fields_ = [("k_pages", ctypes.POINTER(_vp)), ("v_pages", ctypes.POINTER(_vp)), ("num_blocks", _i32)]
+
+
+class KvLayer(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("num_blocks", _i32), ("dtype", _i32)]
+
+
+class ChunkBatch(ctypes.Structure):
+    _fields_ = [("starts", _vp), ("context_lens", _vp), ("block_table", _vp), ("max_blocks", _i32), ("B", _i32),
+                ("rows", _i32), ("max_chunk", _i32)]
 
 
 class PlannerConfig(ctypes.Structure):
@@ -105,6 +116,16 @@ _SIGS = {
                                             _vp, _i32, _i32, _vp, _vp, _sz, _vp]),
     "nightjar_accept_noalloc": (ctypes.c_int, [ctypes.POINTER(ModelDesc), _vp, _vp, _vp, _vp, _i32, _i32, _vp, _vp,
                                                _vp, _vp]),
+    "nightjar_chunk_attn_workspace_bytes": (_sz, [ctypes.POINTER(ModelDesc), _i32, _i32, _i32]),
+    "nightjar_chunk_store": (ctypes.c_int, [ctypes.POINTER(ModelDesc), ctypes.POINTER(KvLayer),
+                                            ctypes.POINTER(ChunkBatch), _vp, ctypes.c_int64, _vp, _vp, _sz, _vp]),
+    "nightjar_chunk_load": (ctypes.c_int, [ctypes.POINTER(ModelDesc), ctypes.POINTER(KvLayer),
+                                           ctypes.POINTER(ChunkBatch), _vp, _vp, _vp, _sz, _vp]),
+    "nightjar_chunk_attn": (ctypes.c_int, [ctypes.POINTER(ModelDesc), ctypes.POINTER(KvLayer),
+                                           ctypes.POINTER(ChunkBatch), _vp, _vp, _vp, _sz, _vp]),
+    "nightjar_sample_workspace_bytes": (_sz, [_i32, _i32]),
+    "nightjar_sample": (ctypes.c_int, [_vp, ctypes.c_int64, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                       ctypes.c_int64, _vp, _sz, _vp]),
     "nightjar_planner_create": (_vp, [ctypes.POINTER(PlannerConfig)]),
     "nightjar_planner_destroy": (None, [_vp]),
     "nightjar_planner_set_switch_cost": (ctypes.c_int, [_vp, _vp, _i32, _vp, _i32, _vp]),
@@ -290,6 +311,41 @@ def attn_verify(desc, q, k_pages, v_pages, num_blocks, win_k, win_v, block_table
     _check(lib().nightjar_attn_verify(ctypes.byref(desc), q, k_pages, v_pages, num_blocks, win_k, win_v,
                                       block_table, max_blocks, context_lens, B, k, out, workspace, workspace_nbytes,
                                       stream))
+
+
+def chunk_attn_workspace_bytes(desc, B, rows, max_chunk) -> int:
+    n = lib().nightjar_chunk_attn_workspace_bytes(ctypes.byref(desc), B, rows, max_chunk)
+    if n == 0:
+        raise NightjarError(NJ_EINVAL, last_error())
+    return n
+
+
+def chunk_store(desc, kv, batch, qkv, qkv_stride, q_out, workspace, workspace_nbytes, stream: int = 0) -> None:
+    _check(lib().nightjar_chunk_store(ctypes.byref(desc), ctypes.byref(kv), ctypes.byref(batch), qkv, qkv_stride,
+                                      q_out, workspace, workspace_nbytes, stream))
+
+
+def chunk_load(desc, kv, batch, k_out, v_out, workspace, workspace_nbytes, stream: int = 0) -> None:
+    _check(lib().nightjar_chunk_load(ctypes.byref(desc), ctypes.byref(kv), ctypes.byref(batch), k_out, v_out,
+                                     workspace, workspace_nbytes, stream))
+
+
+def chunk_attn(desc, kv, batch, q, out, workspace, workspace_nbytes, stream: int = 0) -> None:
+    _check(lib().nightjar_chunk_attn(ctypes.byref(desc), ctypes.byref(kv), ctypes.byref(batch), q, out, workspace,
+                                     workspace_nbytes, stream))
+
+
+def sample_workspace_bytes(rows, vocab) -> int:
+    n = lib().nightjar_sample_workspace_bytes(rows, vocab)
+    if n == 0:
+        raise NightjarError(NJ_EINVAL, last_error())
+    return n
+
+
+def sample(logits, logits_stride, rows, vocab, temperature, top_k, top_p, min_p, uniforms, tokens, probs, probs_stride,
+           workspace, workspace_nbytes, stream: int = 0) -> None:
+    _check(lib().nightjar_sample(logits, logits_stride, rows, vocab, temperature, top_k, top_p, min_p, uniforms, tokens,
+                                 probs, probs_stride, workspace, workspace_nbytes, stream))
 
 
 def packed_weight_elems(N, K) -> int:

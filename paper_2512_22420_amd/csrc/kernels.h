@@ -313,6 +313,14 @@ struct KvAppendArgs {
 };
 hipError_t launch_kv_append(const KvAppendArgs& a, hipStream_t s);
 
+// Ragged chunks over a paged cache (chunk.h).  pages: kPageF32 / kPageBF16 /
+// kPageE4M3; the last two are D = 128 with bf16 rows.
+struct ChunkK;
+hipError_t launch_chunk_store(const ChunkK& a, int pages, const float* qkv, int64_t stride, int H, int Hkv, int D,
+                              float theta, void* q_out, void* k, void* v, void* ks, void* vs, hipStream_t s);
+hipError_t launch_chunk_load(const ChunkK& a, int pages, int Hkv, int D, const void* k, const void* v, const void* ks,
+                             const void* vs, void* k_out, void* v_out, hipStream_t s);
+
 hipError_t launch_fill_i32(int32_t* p, int32_t v, int n, hipStream_t s);
 hipError_t launch_copy_i32(int32_t* dst, const int32_t* src, int n, hipStream_t s);
 // dst[i] = src[i * stride] for 32-bit words, i < n.

@@ -140,3 +140,130 @@ def kv_append(model: DeviceModel, cache: DeviceCache, io: StepIO, ws: Workspace,
 def device_error(ws: Workspace, stream: Optional[int] = None) -> int:
     s = torch.cuda.current_stream().cuda_stream if stream is None else stream
     return nb.device_error(ws.ptr, ws.nbytes, s)
+
+
+class KvLayer:
+    """One layer's paged cache for the chunk calls: k [num_blocks][Hkv][16][D] and
+    v [num_blocks][Hkv][D][16], fp32, bf16 (or its bits as int16), or e4m3 codes
+    as uint8 with a scale byte per (block, head, slot)."""
+
+    _DTYPES = {torch.float32: nb.NJ_F32, torch.bfloat16: nb.NJ_BF16, torch.int16: nb.NJ_BF16, torch.uint8: nb.NJ_E4M3}
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                 v_scale: Optional[torch.Tensor] = None):
+        if k.dtype not in self._DTYPES or v.dtype != k.dtype or k.dim() != 4 or v.dim() != 4:
+            raise TypeError("k and v: need 4-d tensors of one page type (float32, bfloat16 or int16 bits, uint8 codes)")
+        nb_, hkv, bs, D = k.shape
+        if tuple(v.shape) != (nb_, hkv, D, bs):
+            raise TypeError(f"v: need shape {(nb_, hkv, D, bs)}, got {tuple(v.shape)}")
+        for t, n in ((k, "k"), (v, "v")):
+            _expect(t, k.dtype, nb_ * hkv * bs * D, n)
+        if (k.dtype == torch.uint8) != (k_scale is not None) or (k_scale is None) != (v_scale is None):
+            raise TypeError("k_scale and v_scale: needed for e4m3 pages, and for no others")
+        for t, n in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            _expect(t, torch.uint8, nb_ * hkv * bs, n)
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.hkv, self.head_dim = hkv, D
+        self.c = nb.KvLayer(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), nb_, self._DTYPES[k.dtype])
+
+
+class ChunkBatch:
+    """A ragged batch of chunks (nj_chunk_batch)."""
+
+    def __init__(self, starts: torch.Tensor, context_lens: torch.Tensor, block_table: torch.Tensor, rows: int,
+                 max_chunk: int):
+        B = context_lens.numel()
+        _expect(starts, torch.int32, B + 1, "starts")
+        _expect(context_lens, torch.int32, B, "context_lens")
+        _expect(block_table, torch.int32, B * block_table.shape[-1], "block_table")
+        self.starts, self.context_lens, self.block_table = starts, context_lens, block_table
+        self.B, self.rows, self.max_chunk = B, rows, max_chunk
+        self.c = nb.ChunkBatch(_ptr(starts), _ptr(context_lens), _ptr(block_table), block_table.shape[-1], B, rows,
+                               max_chunk)
+
+
+class Scratch:
+    """A caller-owned workspace, prepared for its calls."""
+
+    def __init__(self, nbytes: int, device="cuda", stream: Optional[int] = None):
+        self.nbytes = nbytes
+        self.buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        self.ptr = self.buf.data_ptr()
+        nb.workspace_init(self.ptr, nbytes, torch.cuda.current_stream().cuda_stream if stream is None else stream)
+
+
+def chunk_workspace(desc, batch: ChunkBatch, device="cuda", stream: Optional[int] = None) -> Scratch:
+    """A workspace for the chunk calls on this batch and every smaller one."""
+    return Scratch(nb.chunk_attn_workspace_bytes(desc, batch.B, batch.rows, batch.max_chunk), device, stream)
+
+
+def sample_workspace(rows: int, vocab: int, device="cuda", stream: Optional[int] = None) -> Scratch:
+    return Scratch(nb.sample_workspace_bytes(rows, vocab), device, stream)
+
+
+def _expect_row(t: torch.Tensor, desc, numel: int, name: str) -> None:
+    if desc.dtype == nb.NJ_F32:
+        _expect(t, torch.float32, numel, name)
+    else:
+        _expect(t, torch.int16 if t.dtype == torch.int16 else torch.bfloat16, numel, name)
+
+
+def _expect_layer(desc, layer: KvLayer) -> None:
+    if (layer.hkv, layer.head_dim) != (desc.n_kv_heads, desc.head_dim):
+        raise TypeError(f"cache: need {desc.n_kv_heads} KV heads of {desc.head_dim} dims, got {layer.hkv} of {layer.head_dim}")
+
+
+def chunk_store(desc, layer: KvLayer, batch: ChunkBatch, qkv: torch.Tensor, ws: Scratch,
+                q_out: Optional[torch.Tensor] = None, stream: Optional[int] = None):
+    """RoPE on the chunk's q and k, its K and V into the pages (nightjar_chunk_store).  qkv: fp32
+    [rows, (H + 2 Hkv) * D], rows may be strided."""
+    width = (desc.n_heads + 2 * desc.n_kv_heads) * desc.head_dim
+    if qkv.dtype != torch.float32 or tuple(qkv.shape) != (batch.rows, width) or qkv.stride(1) != 1:
+        raise TypeError(f"qkv: need a float32 tensor [{batch.rows}, {width}] with contiguous rows, got {qkv.dtype} {tuple(qkv.shape)}")
+    _expect_layer(desc, layer)
+    if q_out is not None:
+        _expect_row(q_out, desc, batch.rows * desc.n_heads * desc.head_dim, "q_out")
+    s = torch.cuda.current_stream().cuda_stream if stream is None else stream
+    nb.chunk_store(desc, layer.c, batch.c, qkv.data_ptr(), qkv.stride(0) if batch.rows > 1 else width, _ptr(q_out),
+                   ws.ptr, ws.nbytes, s)
+
+
+def chunk_load(desc, layer: KvLayer, batch: ChunkBatch, k_out: torch.Tensor, v_out: torch.Tensor, ws: Scratch,
+               stream: Optional[int] = None):
+    """The chunk's K and V rows read back from the pages (nightjar_chunk_load)."""
+    _expect_layer(desc, layer)
+    for t, n in ((k_out, "k_out"), (v_out, "v_out")):
+        _expect_row(t, desc, batch.rows * desc.n_kv_heads * desc.head_dim, n)
+    s = torch.cuda.current_stream().cuda_stream if stream is None else stream
+    nb.chunk_load(desc, layer.c, batch.c, k_out.data_ptr(), v_out.data_ptr(), ws.ptr, ws.nbytes, s)
+
+
+def chunk_attn(desc, layer: KvLayer, batch: ChunkBatch, q: torch.Tensor, out: torch.Tensor, ws: Scratch,
+               stream: Optional[int] = None):
+    """Attention of the chunk's rows over the paged cache (nightjar_chunk_attn)."""
+    _expect_layer(desc, layer)
+    for t, n in ((q, "q"), (out, "out")):
+        _expect_row(t, desc, batch.rows * desc.n_heads * desc.head_dim, n)
+    s = torch.cuda.current_stream().cuda_stream if stream is None else stream
+    nb.chunk_attn(desc, layer.c, batch.c, q.data_ptr(), out.data_ptr(), ws.ptr, ws.nbytes, s)
+
+
+def sample(logits: torch.Tensor, uniforms: torch.Tensor, tokens: torch.Tensor, ws: Scratch,
+           temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+           top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None,
+           probs: Optional[torch.Tensor] = None, stream: Optional[int] = None):
+    """One token per row of logits (nightjar_sample).  logits and probs: fp32 [rows, vocab], rows may be strided."""
+    if logits.dim() != 2:
+        raise TypeError(f"logits: need [rows, vocab], got {tuple(logits.shape)}")
+    R, V = logits.shape
+    for t, n in ((logits, "logits"), (probs, "probs")):
+        if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (R, V) or (V > 1 and t.stride(1) != 1)):
+            raise TypeError(f"{n}: need a float32 tensor [{R}, {V}] with contiguous rows, got {t.dtype} {tuple(t.shape)}")
+    for t, n in ((uniforms, "uniforms"), (temperature, "temperature"), (top_p, "top_p"), (min_p, "min_p")):
+        _expect(t, torch.float32, R, n)
+    _expect(tokens, torch.int32, R, "tokens")
+    _expect(top_k, torch.int32, R, "top_k")
+    s = torch.cuda.current_stream().cuda_stream if stream is None else stream
+    nb.sample(logits.data_ptr(), logits.stride(0) if R > 1 else V, R, V, _ptr(temperature), _ptr(top_k), _ptr(top_p),
+              _ptr(min_p), _ptr(uniforms), _ptr(tokens), _ptr(probs), 0 if probs is None else probs.stride(0) if R > 1 else V,
+              ws.ptr, ws.nbytes, s)

@@ -1,0 +1,327 @@
+"""Chunks of new tokens on the GPU: their keys and values written to the paged
+cache (fp32, bf16, e4m3) and read back, and their attention over it, against
+64-bit references.  The pool around the tokens is filled with NaN (or NaN codes
+and scales), so that any read of a slot that is not the sequence's shows."""
+import dataclasses
+
+import numpy as np
+import pytest
+import torch
+
+import serve_ref as ref
+from paper_2512_22420_amd import binding as nb
+from paper_2512_22420_amd import workload as W
+from paper_2512_22420_amd.device import (ChunkBatch, KvLayer, Scratch, chunk_attn, chunk_load, chunk_store,
+                                        chunk_workspace, device_error, model_desc)
+
+pytestmark = pytest.mark.gpu
+
+
+def _shape(H, Hkv, dtype="bf16", D=128):
+    return dataclasses.replace(W.LLAMA8B_LAYER if dtype == "bf16" else W.TINY_F32, n_heads=H, n_kv_heads=Hkv, head_dim=D, dtype=dtype)
+
+
+L8, L7, MHA, MQA = _shape(32, 8), _shape(28, 4), _shape(2, 2), _shape(16, 1)
+TF = W.TINY_F32
+TD = {"f32": torch.float32, "bf16": torch.bfloat16, "e4m3": torch.uint8}
+
+
+def _dev(a, dtype=torch.int32):
+    return torch.as_tensor(np.ascontiguousarray(a)).to("cuda", dtype)
+
+
+class Case:
+    """A batch of chunks with a NaN-filled pool."""
+
+    def __init__(self, shape, pages, n, ctx, seed=0, tail=0, lead=0, max_chunk=None):
+        self.shape, self.pages, self.rng = shape, pages, np.random.default_rng(seed)
+        self.n, self.ctx = np.asarray(n), np.asarray(ctx)
+        self.starts = lead + np.concatenate([[0], np.cumsum(self.n)])
+        self.rows = int(self.starts[-1]) + tail
+        self.total = self.n + self.ctx
+        need = np.maximum(1, -(-self.total // 16))
+        self.pool = int(need.sum()) + 3
+        perm = self.rng.permutation(self.pool)
+        self.table = np.full((len(n), int(need.max()) + 1), -1, np.int32)
+        at = 0
+        for b, k in enumerate(need):
+            self.table[b, :k] = perm[at:at + k]
+            at += k
+        s = shape
+        kt = TD[pages]
+        fill = 0x7F if pages == "e4m3" else float("nan")
+        self.k = torch.full((self.pool, s.n_kv_heads, 16, s.head_dim), fill, dtype=kt, device="cuda")
+        self.v = torch.full((self.pool, s.n_kv_heads, s.head_dim, 16), fill, dtype=kt, device="cuda")
+        self.ks = torch.full((self.pool, s.n_kv_heads, 16), 255, dtype=torch.uint8, device="cuda") if pages == "e4m3" else None
+        self.vs = self.ks.clone() if pages == "e4m3" else None
+        self.desc = model_desc(s)
+        self.layer = KvLayer(self.k, self.v, self.ks, self.vs)
+        self.batch = ChunkBatch(_dev(self.starts), _dev(self.ctx), _dev(self.table), self.rows, max_chunk or max(1, int(self.n.max())))
+        self.ws = chunk_workspace(self.desc, self.batch)
+        self.rdt = torch.float32 if s.dtype == "f32" else torch.bfloat16
+
+    def fill_context(self, first=None):
+        """Writes positions 0 .. first-1 (default: all tokens) of every sequence; returns their values, float64, by sequence."""
+        s, first = self.shape, self.total if first is None else first
+        vals = []
+        for b, c in enumerate(first):
+            k = self.rng.normal(size=(c, s.n_kv_heads, s.head_dim)) * 0.8
+            v = self.rng.normal(size=(c, s.n_kv_heads, s.head_dim)) * 0.5
+            k, v = torch.as_tensor(k, dtype=torch.float32), torch.as_tensor(v, dtype=torch.float32)
+            if c:
+                blk, slot = torch.as_tensor(self.table[b].astype(np.int64))[torch.arange(c) // 16].cuda(), (torch.arange(c) % 16).cuda()
+                if self.pages == "e4m3":
+                    for x, pages, sc in ((k, self.k, self.ks), (v, self.v.transpose(2, 3), self.vs)):
+                        e = torch.as_tensor(ref.scale_exp(x.numpy()))
+                        codes = (x * 2.0 ** -e[..., None]).to(torch.float8_e4m3fn).view(torch.uint8)
+                        pages[blk, :, slot] = codes.cuda()
+                        sc[blk, :, slot] = (e + 127).to(torch.uint8).cuda()
+                else:
+                    self.k[blk, :, slot] = k.to(self.k.dtype).cuda()
+                    self.v.transpose(2, 3)[blk, :, slot] = v.to(self.v.dtype).cuda()
+            vals.append(self.values(b, c))
+        return vals
+
+    def values(self, b, c):
+        """K and V [c, Hkv, D] of sequence b's first c tokens as they stand in the pages."""
+        blk, slot = self.table[b].astype(np.int64)[np.arange(c) // 16], np.arange(c) % 16
+        k, v = self.k.cpu(), self.v.transpose(2, 3).cpu()
+        if self.pages == "e4m3":
+            k, v = (ref.decode(x.numpy()[blk, :, slot], sc.cpu().numpy()[blk, :, slot]) for x, sc in ((k, self.ks), (v, self.vs)))
+            return k, v
+        return k.double().numpy()[blk, :, slot], v.double().numpy()[blk, :, slot]
+
+    def error(self):
+        return device_error(self.ws)
+
+
+BATCHES = [  # new tokens, cached tokens
+    ([1], [0]), ([1, 1, 1], [0, 16, 47]), ([5, 0, 20], [3, 9, 0]), ([16, 32], [0, 16]), ([40, 1, 17, 0, 0, 3], [15, 100, 1, 7, 0, 31]),
+    ([1] * 70, list(range(70))), ([130], [1000]),
+]
+
+
+@pytest.mark.parametrize("pages,shape", [("e4m3", L8), ("bf16", L7), ("e4m3", MHA), ("f32", TF), ("f32", _shape(3, 1, "f32", 24))],
+                         ids=["e4m3-8b", "bf16-7b", "e4m3-mha", "f32-tiny", "f32-d24"])
+@pytest.mark.parametrize("n,ctx", BATCHES, ids=range(len(BATCHES)))
+@pytest.mark.parametrize("stride_pad", [0, 12])
+def test_store_and_load(pages, shape, n, ctx, stride_pad):
+    c = Case(shape, pages, n, ctx, seed=len(n), tail=3, lead=2)
+    s = shape
+    nh = s.n_heads + 2 * s.n_kv_heads
+    x = c.rng.normal(size=(c.rows, nh, s.head_dim)).astype(np.float32)
+    x[:, s.n_heads:, ::7] *= 20
+    buf = torch.full((c.rows, nh * s.head_dim + stride_pad), float("nan"), device="cuda")
+    buf[:, :nh * s.head_dim] = torch.as_tensor(x).view(c.rows, -1).cuda()
+    qkv = buf[:, :nh * s.head_dim]
+    q_out = torch.full((c.rows, s.n_heads, s.head_dim), -7.0, dtype=c.rdt, device="cuda")
+    k0, v0 = c.k.cpu().clone(), c.v.cpu().clone()
+    chunk_store(c.desc, c.layer, c.batch, qkv, c.ws, q_out=q_out)
+    k_out, v_out = (torch.full((c.rows, s.n_kv_heads, s.head_dim), -7.0, dtype=c.rdt, device="cuda") for _ in range(2))
+    chunk_load(c.desc, c.layer, c.batch, k_out, v_out, c.ws)
+    assert c.error() == 0
+
+    seq, pos = ref.places(c.starts, c.ctx)
+    own = slice(c.starts[0], c.starts[-1])
+    qk = ref.rotate(x[own, :s.n_heads + s.n_kv_heads], pos, s.rope_theta).astype(np.float32)
+    q, k, v = qk[:, :s.n_heads], qk[:, s.n_heads:], x[own, s.n_heads + s.n_kv_heads:]
+    got_q, got_k, got_v = (t.float().cpu().numpy() for t in (q_out, k_out, v_out))
+    for t in (got_q, got_k, got_v):  # rows that are nobody's
+        assert (t[:c.starts[0]] == -7).all() and (t[c.starts[-1]:] == -7).all()
+    # fp32 results may differ in the last bit, and where that moves a rounding, by a step of the narrower type
+    step = {"f32": 2.0 ** -23, "bf16": 2.0 ** -7}
+    row_t = "f32" if s.dtype == "f32" else "bf16"
+
+    def near(got, want, kind, border=None):
+        want_t = torch.as_tensor(want).to(TD[kind] if kind != "e4m3" else torch.float32).float().numpy()
+        diff = got != want_t
+        assert (np.abs(got - want_t)[diff] <= step[kind] * np.abs(want_t)[diff] * 1.01).all()
+        assert diff.mean() < (0.2 if kind == "f32" else 1e-4)
+    near(got_q[own], q, row_t)
+    if pages == "e4m3":
+        for got, x32, sc in ((got_k[own], k, c.ks), (got_v[own], v, c.vs)):
+            want, scale, border = ref.encode(x32)
+            bad = got != want
+            assert (border[bad] < 1e-6).all()
+            blk = c.table[seq, pos // 16]
+            assert np.array_equal(sc.cpu().numpy()[blk, :, pos % 16], scale)
+    else:
+        near(got_k[own], k, row_t)
+        assert np.array_equal(got_v[own], torch.as_tensor(v).to(c.rdt).float().numpy())
+    # nothing but the tokens' own slots has changed
+    mine = np.zeros((c.pool, 16), bool)
+    mine[c.table[seq, pos // 16], pos % 16] = True
+    for after, before, at in ((c.k, k0, (0, 2)), (c.v, v0, (0, 3))):
+        d = after.cpu().contiguous().view(torch.uint8 if pages == "e4m3" else torch.int32 if pages == "f32" else torch.int16).numpy() != \
+            before.contiguous().view(torch.uint8 if pages == "e4m3" else torch.int32 if pages == "f32" else torch.int16).numpy()
+        changed = d.any(axis=tuple(i for i in range(4) if i not in at))
+        assert not (changed & ~mine).any()
+    if pages == "e4m3":
+        for sc in (c.ks, c.vs):
+            assert not ((sc.cpu().numpy() != 255).any(1) & ~mine).any()
+
+
+def test_store_special_values():
+    """Zeros, the scale's two ends, exact borders, NaN and infinities (V is stored without rotation)."""
+    s = MHA
+    c = Case(s, "e4m3", [7], [0])
+    x = np.zeros((7, 6, 128), np.float32)
+    v = x[:, 4:]
+    v[1] = np.linspace(-448, 448, 128)
+    v[2, :, 0], v[2, :, 1] = 3.0e38, -1.0       # the scale's upper end: saturated, small values lost
+    v[3] = 2.0 ** -115                           # the lower end
+    v[4, :, ::3], v[4, :, 1::3], v[4, :, 2::3] = np.nan, np.inf, 5.0
+    v[5, :, 0], v[5, :, 1:] = 448.0, np.arange(1, 128) + 0.5
+    v[6, :, 0] = 448.0001 * 2.0 ** 20            # just above a power's limit
+    chunk_store(c.desc, c.layer, c.batch, torch.as_tensor(x).view(7, -1).cuda(), c.ws)
+    k_out, v_out = (torch.empty((7, 2, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    chunk_load(c.desc, c.layer, c.batch, k_out, v_out, c.ws)
+    assert c.error() == 0
+    want, scale, _ = ref.encode(v)
+    got = v_out.float().cpu().numpy()
+    assert np.array_equal(got, want.astype(np.float32), equal_nan=True)
+    blk = c.table[0, 0]
+    assert np.array_equal(c.vs.cpu().numpy()[blk, :, :7].T, scale)
+    assert (k_out == 0).all() and (c.ks[blk, :, :7] == 15).all()
+
+
+def test_bad_batches_are_flagged_and_skipped():
+    s = MHA
+    for starts, ctx, max_chunk, ids, bits in (
+            ([0, 4, 9], [0, -1], 5, None, nb.NJ_DEV_BAD_CONTEXT), ([0, 4, 9], [0, 1000], 5, None, nb.NJ_DEV_BAD_CONTEXT),
+            ([0, 4, 9], [0, 2 ** 31 - 1], 5, None, nb.NJ_DEV_BAD_CONTEXT), ([0, 4, 9], [0, 0], 4, None, nb.NJ_DEV_BAD_CONTEXT),
+            ([0, 4, 2], [0, 0], 5, None, nb.NJ_DEV_BAD_CONTEXT), ([0, 4, 99], [0, 0], 9, None, nb.NJ_DEV_BAD_CONTEXT),
+            ([-5, 4, 9], [0, 0], 9, None, nb.NJ_DEV_BAD_CONTEXT), ([0, 4, 9], [0, 0], 5, -1, nb.NJ_DEV_BAD_BLOCK),
+            ([0, 4, 9], [0, 0], 5, 10 ** 6, nb.NJ_DEV_BAD_BLOCK)):
+        for pages, shape in (("e4m3", s), ("bf16", s), ("f32", _shape(2, 2, "f32", 64))):
+            c = Case(shape, pages, [4, 5], [0, 0], tail=2)
+            good = c.fill_context()
+            if ids is not None:
+                c.table[1] = ids
+            c.batch = ChunkBatch(_dev(starts), _dev(ctx), _dev(c.table), 9, max_chunk)
+            nh = 6 * shape.head_dim
+            k0, v0 = c.k.cpu().clone(), c.v.cpu().clone()
+            q = torch.full((9, 2, shape.head_dim), 0.5, dtype=c.rdt, device="cuda")
+            outs = [torch.full((9, 2, shape.head_dim), -7.0, dtype=c.rdt, device="cuda") for _ in range(3)]
+            chunk_load(c.desc, c.layer, c.batch, outs[0], outs[1], c.ws)
+            assert c.error() == bits, (starts, ctx, pages)
+            chunk_attn(c.desc, c.layer, c.batch, q, outs[2], c.ws)
+            assert c.error() == bits, (starts, ctx, pages)
+            chunk_store(c.desc, c.layer, c.batch, torch.zeros((9, nh), device="cuda"), c.ws, q_out=q)
+            assert c.error() == bits, (starts, ctx, pages)
+            assert c.error() == 0
+            if starts[0] == 0:  # the first sequence is served, the second one's rows and slots are left alone
+                k, v = good[0]
+                assert np.array_equal(outs[0][:4].double().cpu().numpy(), k[:4]) and (outs[0][4:] == -7).all()
+                assert np.array_equal(outs[1][:4].double().cpu().numpy(), v[:4])
+                if bits == nb.NJ_DEV_BAD_CONTEXT:
+                    assert (outs[2][4:] == -7).all() and not (outs[2][:4] == -7).any()
+            kinds = {"e4m3": torch.uint8, "bf16": torch.int16, "f32": torch.int32}
+            served = 0 if starts[0] == 0 else 1  # the other sequence's blocks stay as they were
+            for blk in set(range(c.pool)) - {int(c.table[served, 0])}:
+                for now, was in ((c.k, k0), (c.v, v0)):
+                    assert torch.equal(now[blk].cpu().contiguous().view(kinds[pages]), was[blk].contiguous().view(kinds[pages]))
+
+
+def _check_attn(c, q, out, vals):
+    """Elementwise: with p rounded to bf16 (half a step: 2^-8 relative, each with its own sign) and the output rounded,
+    |error| <= 2^-8 (sum p |v| + |o|); fp32 paths: sums of up to n + D terms.  Both: scores summed in fp32, whose
+    error (D + 2) 2^-24 sum |q k| / sqrt(D) is relative to p, numerator and denominator."""
+    D = c.shape.head_dim
+    qd, got = q.double().cpu().numpy(), out.double().cpu().numpy().reshape(c.rows, c.shape.n_heads, D)
+    for b, (n, ctx) in enumerate(zip(c.n, c.ctx)):
+        r = slice(c.starts[b], c.starts[b + 1])
+        if n == 0:
+            continue
+        o, a, big = ref.attention(qd[r], *vals[b], ctx)
+        half = 2.0 ** -8 if c.rdt == torch.bfloat16 else 0.0
+        soft = 2 * (D + 2) * 2.0 ** -24 * big + (n + ctx + 8) * 2.0 ** -24
+        tol = 1.02 * (half * (a + np.abs(o)) + soft * a) + 2.0 ** -23 * np.abs(o)
+        bad = ~(np.abs(got[r] - o) <= tol)
+        assert not bad.any(), (b, n, ctx, np.argwhere(bad)[:3], got[r][bad][:3], o[bad][:3], tol[bad][:3])
+
+
+ATTN = [([1], [0]), ([1], [16]), ([2, 1, 1], [0, 15, 31]), ([1, 3, 0, 2], [63, 64, 5, 200]), ([17], [0]), ([33, 1], [7, 300]),
+        ([64], [64]), ([100, 1, 31], [0, 511, 96]), ([129], [65]), ([1], [2500]), ([4, 5], [1500, 33]), ([300], [17])]
+
+
+@pytest.mark.parametrize("pages,shape", [("e4m3", L8), ("bf16", L8), ("e4m3", L7), ("bf16", L7), ("bf16", MHA), ("e4m3", MQA),
+                                         ("f32", TF), ("f32", _shape(6, 2, "f32", 24))],
+                         ids=["e4m3-8b", "bf16-8b", "e4m3-7b", "bf16-7b", "bf16-mha", "e4m3-mqa", "f32-tiny", "f32-d24"])
+@pytest.mark.parametrize("n,ctx", ATTN, ids=range(len(ATTN)))
+def test_attention(pages, shape, n, ctx):
+    c = Case(shape, pages, n, ctx, seed=11 + len(n), tail=2, lead=1)
+    vals = c.fill_context()
+    q = torch.as_tensor(c.rng.normal(size=(c.rows, shape.n_heads, shape.head_dim)) * 1.5).to("cuda", c.rdt)
+    out = torch.full((c.rows, shape.n_heads * shape.head_dim), -7.0, dtype=c.rdt, device="cuda")
+    chunk_attn(c.desc, c.layer, c.batch, q, out, c.ws)
+    assert c.error() == 0
+    assert (out[:c.starts[0]] == -7).all() and (out[c.starts[-1]:] == -7).all()
+    _check_attn(c, q, out, vals)
+    again = torch.empty_like(out)
+    chunk_attn(c.desc, c.layer, c.batch, q, again, c.ws)
+    own = slice(c.starts[0], c.starts[-1])
+    assert torch.equal(out[own].view(torch.int16 if c.rdt == torch.bfloat16 else torch.int32),
+                       again[own].view(torch.int16 if c.rdt == torch.bfloat16 else torch.int32))
+
+
+def test_attention_many_decoding_sequences():
+    n, ctx = [1] * 300, [(37 * b) % 90 for b in range(300)]
+    c = Case(_shape(8, 2), "e4m3", n, ctx, seed=5)
+    vals = c.fill_context()
+    q = torch.as_tensor(c.rng.normal(size=(300, 8, 128))).to("cuda", torch.bfloat16)
+    out = torch.empty((300, 1024), dtype=torch.bfloat16, device="cuda")
+    chunk_attn(c.desc, c.layer, c.batch, q, out, c.ws)
+    assert c.error() == 0
+    _check_attn(c, q, out, vals)
+
+
+@pytest.mark.parametrize("pages", ["bf16", "e4m3"])
+def test_attention_peaked_rows(pages):
+    """A key that leads its row by far: the output is that token's value, with the output's rounding only."""
+    c = Case(L8, pages, [40, 1], [100, 700], seed=2)
+    vals = c.fill_context()
+    q = torch.zeros((c.rows, 32, 128), device="cuda", dtype=torch.bfloat16)
+    lead = 57
+    for b in range(2):
+        k = torch.as_tensor(vals[b][0][lead])  # [Hkv, D]
+        q[c.starts[b]:c.starts[b + 1]] = (40 * k).repeat_interleave(4, 0).to("cuda", torch.bfloat16)
+    out = torch.empty((c.rows, 4096), dtype=torch.bfloat16, device="cuda")
+    chunk_attn(c.desc, c.layer, c.batch, q, out, c.ws)
+    for b in range(2):
+        want = np.repeat(vals[b][1][lead], 4, 0)
+        got = out[c.starts[b]:c.starts[b + 1]].double().cpu().numpy().reshape(-1, 32, 128)
+        assert (np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + 1e-6).all()
+
+
+def test_graph_replay_and_other_stream():
+    """Captured and replayed, with eager work between, and on a side stream: the eager result every time."""
+    c = Case(L8, "e4m3", [40, 1, 1, 9], [0, 300, 47, 128], seed=8)
+    c.fill_context(first=c.ctx)
+    nh = 48 * 128
+    qkv = torch.randn((c.rows, nh), device="cuda")
+    q, out = (torch.empty((c.rows, 32, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+
+    def go():
+        chunk_store(c.desc, c.layer, c.batch, qkv, c.ws, q_out=q)
+        chunk_attn(c.desc, c.layer, c.batch, q, out, c.ws)
+    go()
+    want = out.clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        go()
+    for _ in range(3):
+        out.fill_(3.0)
+        q.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        go()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        out.zero_()
+        go()
+    side.synchronize()
+    assert torch.equal(out, want) and c.error() == 0

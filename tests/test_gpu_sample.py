@@ -1,0 +1,164 @@
+"""Sampling on the GPU against the 64-bit reference: the same token, and the
+truncated distribution to fp32 rounding (w / total in 64 bits, rounded once:
+2^-24 relative; the units of 2^-44 that the total is summed in: V 2^-45 of it)."""
+import numpy as np
+import pytest
+import torch
+
+import serve_ref as ref
+from paper_2512_22420_amd import binding as nb
+from paper_2512_22420_amd.device import device_error, sample, sample_workspace
+
+pytestmark = pytest.mark.gpu
+
+
+
+def _run(l, u, T=None, k=None, p=None, m=None, probs=True, pad=0):
+    """Tokens, probabilities and device error bits of logits l [R, V] (numpy fp32)."""
+    R, V = l.shape
+    buf = torch.full((R, V + pad), float("nan"), device="cuda")
+    buf[:, :V] = torch.as_tensor(l).cuda()
+    out = torch.full((R, V + pad), -3.0, device="cuda")
+    tok = torch.full((R,), -9, dtype=torch.int32, device="cuda")
+    ws = sample_workspace(R, V)
+    full = lambda x, dt: None if x is None else torch.as_tensor(np.broadcast_to(np.asarray(x), (R,)).copy()).to("cuda", dt)  # noqa: E731
+    f = torch.float32
+    sample(buf[:, :V], full(u, f), tok, ws, temperature=full(T, f), top_k=full(k, torch.int32), top_p=full(p, f),
+           min_p=full(m, f), probs=out[:, :V] if probs else None)
+    err = device_error(ws)
+    assert (out[:, V:] == -3).all()
+    return tok.cpu().numpy(), out[:, :V].cpu().numpy() if probs else None, err
+
+
+def _check(l, u, T=None, k=None, p=None, m=None, **kw):
+    R, V = l.shape
+    tok, probs, err = _run(l, u, T, k, p, m, **kw)
+    assert err == 0
+    at = lambda x, r, d: d if x is None else np.broadcast_to(np.asarray(x), (R,))[r]  # noqa: E731
+    f = lambda x: float(np.float32(x))  # noqa: E731
+    for r in range(R):
+        t, pr = ref.sample(l[r], f(at(u, r, 0)), f(at(T, r, 1.0)), int(at(k, r, 0)), f(at(p, r, 1.0)), f(at(m, r, 0.0)))
+        assert tok[r] == t, (r, tok[r], t)
+        if probs is not None:
+            assert ((probs[r] > 0) == (pr.astype(np.float32) > 0)).all()
+            assert (np.abs(probs[r] - pr) <= (2.0 ** -23 + V * 2.0 ** -44) * pr + 2.0 ** -149).all()
+
+
+SETTINGS = [dict(), dict(T=0.7), dict(T=0.0), dict(k=1), dict(k=50), dict(p=0.9), dict(p=0.5, T=1.4), dict(m=0.05),
+            dict(k=40, p=0.8), dict(k=300, p=0.95, m=0.01, T=0.9), dict(p=0.0), dict(m=1.0), dict(k=10 ** 6, p=2.0, m=0.0),
+            dict(T=1e-30, p=0.99), dict(T=60.0, k=5), dict(k=-4, T=2.0)]
+
+
+@pytest.mark.parametrize("V,pad", [(1, 0), (2, 3), (5, 0), (255, 1), (257, 0), (2048, 4), (4099, 0), (128256, 0), (152064, 0)])
+@pytest.mark.parametrize("kw", SETTINGS, ids=[str(i) for i in range(len(SETTINGS))])
+def test_settings(V, pad, kw):
+    rng = np.random.default_rng(V + len(kw))
+    R = 3
+    l = (2.2 * rng.standard_normal((R, V))).astype(np.float32)
+    hot = rng.integers(0, V, size=(R, min(40, V)))
+    for r in range(R):
+        l[r, hot[r]] += (7 + 2 * rng.standard_normal(hot.shape[1])).astype(np.float32)
+    _check(l, rng.random(R).astype(np.float32), pad=pad, **kw)
+
+
+@pytest.mark.parametrize("kw", [dict(p=0.97), dict(k=20000), dict(k=20000, p=0.9), dict(p=0.999, T=1.5), dict(k=5000, m=0.2), dict(p=0.7, k=100000)])
+@pytest.mark.parametrize("V", [32000, 128256])
+def test_broad_rows(V, kw):
+    """Flat distributions: far more tokens are kept than a sorted list holds."""
+    rng = np.random.default_rng(V)
+    l = rng.standard_normal((2, V)).astype(np.float32)
+    _check(l, rng.random(2).astype(np.float32), **kw)
+
+
+@pytest.mark.parametrize("kw", [dict(k=3), dict(k=700), dict(k=9000), dict(p=0.5), dict(p=0.25, k=9000), dict(T=0.0), dict(), dict(m=0.5)])
+@pytest.mark.parametrize("V", [100, 5000, 20000])
+def test_ties(V, kw):
+    """Equal logits go by index: all equal, two levels, and logits rounded to bf16 (groups of thousands)."""
+    rng = np.random.default_rng(V)
+    a = np.full(V, 1.5, np.float32)
+    b = np.where(rng.random(V) < 0.5, 2.0, 1.0).astype(np.float32)
+    c = torch.as_tensor(rng.standard_normal(V) * 2).to(torch.bfloat16).float().numpy()
+    d = np.where(rng.random(V) < 0.5, 0.0, -0.0).astype(np.float32)
+    _check(np.stack([a, b, c, d]), np.array([0.3, 0.7, 0.5, 0.9], np.float32), **kw)
+
+
+def test_masked_logits():
+    """-inf is never drawn, whatever top-k asks for; a row with one token left gives it; huge and denormal logits."""
+    V = 3000
+    rng = np.random.default_rng(1)
+    l = rng.standard_normal((6, V)).astype(np.float32)
+    l[0, 5:] = -np.inf
+    l[1, :] = -np.inf
+    l[1, 2999] = -4.0
+    l[2, ::2] = -np.inf
+    l[3] = np.finfo(np.float32).min
+    l[3, 17] = np.finfo(np.float32).max
+    l[4] = np.finfo(np.float32).min  # the type's lowest value in every place: a uniform row
+    l[5] *= 1e-40
+    u = rng.random(6).astype(np.float32)
+    for kw in (dict(), dict(k=10), dict(p=0.5), dict(k=10 ** 5, p=0.999), dict(T=0.0), dict(m=0.3)):
+        _check(l, u, **kw)
+
+
+def test_uniforms_at_the_ends():
+    rng = np.random.default_rng(2)
+    l = (3 * rng.standard_normal((4, 500))).astype(np.float32)
+    for kw in (dict(), dict(k=20), dict(p=0.9)):
+        _check(l, np.array([0.0, 1 - 2.0 ** -24, 2.0 ** -149, 0.5], np.float32), **kw)
+
+
+def test_rows_that_cannot_be_sampled():
+    V = 700
+    rng = np.random.default_rng(4)
+    good = rng.standard_normal(V).astype(np.float32)
+    rows, nan, inf = [], np.float32(np.nan), np.float32(np.inf)
+    for j in (0, 300, 699):
+        rows.append(good.copy())
+        rows[-1][j] = nan
+        rows.append(good.copy())
+        rows[-1][j] = inf
+    rows.append(np.full(V, -inf))
+    l = np.stack(rows + [good])
+    tok, probs, err = _run(l, np.full(len(l), 0.4, np.float32))
+    assert err == nb.NJ_DEV_BAD_SAMPLING and (tok[:-1] == -1).all() and (probs[:-1] == 0).all()
+    assert tok[-1] == ref.sample(good, float(np.float32(0.4)))[0]
+    for kw in (dict(T=-1.0), dict(T=nan), dict(T=inf), dict(p=-0.1), dict(p=nan), dict(m=-0.1), dict(m=1.1), dict(m=nan)):
+        tok, probs, err = _run(good[None], np.float32([0.5]), **kw)
+        assert err == nb.NJ_DEV_BAD_SAMPLING and tok[0] == -1 and (probs == 0).all(), kw
+    for u in (-0.1, 1.0, nan):
+        tok, _, err = _run(good[None], np.float32([u]), probs=False)
+        assert err == nb.NJ_DEV_BAD_SAMPLING and tok[0] == -1
+
+
+def test_rows_of_their_own_settings_and_strides():
+    rng = np.random.default_rng(6)
+    R, V = 70, 6001
+    l = (2 * rng.standard_normal((R, V))).astype(np.float32)
+    _check(l, rng.random(R).astype(np.float32), T=rng.choice([0.0, 0.6, 1.0, 1.7], R), k=rng.choice([0, 1, 7, 900, 5000], R),
+           p=rng.choice([1.0, 0.3, 0.9, 0.99], R), m=rng.choice([0.0, 0.02, 0.4], R), pad=3)
+
+
+def test_graph_replay():
+    rng = np.random.default_rng(9)
+    R, V = 5, 128256
+    l = torch.as_tensor((2 * rng.standard_normal((R, V))).astype(np.float32)).cuda()
+    u, p = torch.rand(R, device="cuda"), torch.full((R,), 0.9, device="cuda")
+    tok, probs, ws = torch.empty(R, dtype=torch.int32, device="cuda"), torch.empty_like(l), sample_workspace(R, V)
+
+    def go():
+        sample(l, u, tok, ws, top_p=p, probs=probs)
+    go()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        go()
+    for i in range(3):
+        u.uniform_()
+        go()
+        want = (tok.clone(), probs.clone())
+        tok.zero_()
+        probs.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(tok, want[0]) and torch.equal(probs, want[1])
+    assert device_error(ws) == 0
