@@ -1,6 +1,9 @@
 // Attention of a chunk of new tokens over a paged cache: row i of a sequence
 // sees positions 0 .. c + i, all of them in the pages.
+#include <limits.h>
+
 #include <algorithm>
+#include <type_traits>
 
 #include "../../include/nightjar_serve.h"
 #include "chunk.h"
@@ -8,6 +11,9 @@
 
 namespace nj {
 namespace {
+
+constexpr int kHD = 128;  // head dim of the bf16 path
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 struct ChunkAttnK {
   ChunkK c;
@@ -19,7 +25,218 @@ struct ChunkAttnK {
   void* out;
   int H, Hkv, D;
   float scale_log2;
+  int threshold;      // sequences of more than this many query rows per KV head are cut into tiles, others streamed
+  float* part_o[2];   // per class: [slot][rows of the class][kHD], unnormalised
+  float2* part_ml[2]; // [slot][rows]: max (log2 domain), sum
 };
+
+// ---------------------------------------------------------------------------
+// Work.  A sequence's query rows for one KV head are its n tokens times the G
+// heads that share it, tokens first.  Class kTiles cuts them into tiles of up to
+// 128 rows (whole tokens), class kStream takes sequences of up to 32 rows whole.
+// When a class has fewer pieces than the chip takes, the keys of each piece are
+// cut too, and a merge joins the parts: the cut length L is the same for all
+// sequences of the class, the smallest of maxlen / 1, 2, 3, 4, 6, .. whose pieces
+// still fit kSlots.  Every workgroup works this out by itself from starts and
+// context lengths (a few loads per 64 sequences) instead of reading a list that
+// another kernel would have to write first.
+// ---------------------------------------------------------------------------
+enum { kTiles = 0, kStream = 1 };
+constexpr int kTileRows = 128, kStreamRows = 32;
+constexpr int kSlots[2] = {512, 1024};      // pieces (over all KV heads) up to which keys are cut
+constexpr int kMinCut[2] = {256, 128};      // tokens
+constexpr int kCuts = 12;
+__device__ constexpr int kCutBy[kCuts] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+
+struct Piece {
+  ChunkSeq s;
+  int tile;          // first token tile * tokens
+  int split, nsplit;
+  int slot;          // of split 0 (nsplit > 1)
+  int b;
+};
+
+__device__ __forceinline__ int wave_sum_i(int v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+__device__ __forceinline__ int wave_max_i(int v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = max(v, __shfl_xor(v, o));
+  return v;
+}
+__device__ __forceinline__ int wave_scan_i(int v) {  // inclusive
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const int up = __shfl_up(v, o);
+    if (lane >= o) v += up;
+  }
+  return v;
+}
+
+// Tiles of a sequence in class C (0: not of this class).
+template <int C>
+__device__ __forceinline__ int class_tiles(const ChunkAttnK& a, const ChunkSeq& s, int G, int tokens) {
+  if (s.n == 0 || (s.n * G > a.threshold) != (C == kTiles)) return 0;
+  return C == kTiles ? (s.n + tokens - 1) / tokens : 1;
+}
+
+// Piece `item` of class C (per KV head), or with by_tile the split tile number
+// `item`, with slot and nsplit of all its pieces.  Run by whole waves, the same
+// in each; false if there is none.
+template <int C>
+__device__ bool find_piece(const ChunkAttnK& a, int item, bool by_tile, Piece& out) {
+  const int lane = threadIdx.x & 63, G = a.H / a.Hkv, B = a.c.B, tokens = kTileRows / G;
+  const int cap = kSlots[C] / a.Hkv;
+  // total tiles and the longest key range of the class
+  int tiles = 0, longest = 0;
+  ChunkSeq s0{0, 0, 0, false};
+  int t0 = 0;
+  for (int b0 = 0; b0 < B; b0 += kWave) {
+    const int b = b0 + lane;
+    const ChunkSeq s = b < B ? chunk_seq(a.c, b) : ChunkSeq{0, 0, 0, false};
+    const int t = class_tiles<C>(a, s, G, tokens);
+    if (b0 == 0) {
+      s0 = s;
+      t0 = t;
+    }
+    tiles += t;
+    longest = max(longest, t ? s.c + s.n : 0);
+  }
+  tiles = wave_sum_i(tiles);
+  longest = wave_max_i(longest);
+  if (tiles == 0) return false;
+  // the cut
+  int L = longest;
+  if (tiles * 2 <= cap) {
+    int cnt[kCuts] = {};
+    for (int b0 = 0; b0 < B; b0 += kWave) {
+      const int b = b0 + lane;
+      const ChunkSeq s = b0 == 0 ? s0 : b < B ? chunk_seq(a.c, b) : ChunkSeq{0, 0, 0, false};
+      const int t = b0 == 0 ? t0 : class_tiles<C>(a, s, G, tokens);
+      if (t) {
+#pragma unroll
+        for (int k = 1; k < kCuts; ++k) {
+          const int l = max((longest + kCutBy[k] - 1) / kCutBy[k], kMinCut[C]);
+          cnt[k] += t * ((s.c + s.n + l - 1) / l);
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 1; k < kCuts; ++k)
+      if (wave_sum_i(cnt[k]) <= cap) L = max((longest + kCutBy[k] - 1) / kCutBy[k], kMinCut[C]);
+  }
+  // the piece
+  int before = 0, slots = 0;
+  for (int b0 = 0; b0 < B; b0 += kWave) {
+    const int b = b0 + lane;
+    const ChunkSeq s = b0 == 0 ? s0 : b < B ? chunk_seq(a.c, b) : ChunkSeq{0, 0, 0, false};
+    const int t = b0 == 0 ? t0 : class_tiles<C>(a, s, G, tokens);
+    const int ns = t ? (s.c + s.n + L - 1) / L : 0;
+    const int sl = ns > 1 ? t * ns : 0, mine = by_tile ? (ns > 1 ? t : 0) : t * ns;
+    const int inc = wave_scan_i(mine), sinc = wave_scan_i(sl);
+    const uint64_t hit = __ballot(before + inc > item);
+    if (hit) {
+      // (the same in every lane: kept in scalar registers)
+      const int l = __builtin_amdgcn_readfirstlane(__ffsll((long long)hit) - 1);
+      auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+      const int at = item - (before + of(inc - mine)), nt = of(t);
+      out.b = b0 + l;
+      out.s = {of(s.s0), of(s.n), of(s.c), false};
+      out.nsplit = of(ns);
+      // the last tiles see the most keys: they go first
+      const int rank = by_tile ? at : at / out.nsplit;
+      out.tile = __builtin_amdgcn_readfirstlane(nt - 1 - rank);
+      out.split = __builtin_amdgcn_readfirstlane(by_tile ? 0 : at % out.nsplit);
+      out.slot = __builtin_amdgcn_readfirstlane(slots + of(sinc - sl) + rank * out.nsplit);
+      return true;
+    }
+    before += __builtin_amdgcn_readlane(inc, 63);
+    slots += __builtin_amdgcn_readlane(sinc, 63);
+  }
+  return false;
+}
+
+// Keys of split `split` of a piece that sees `len` keys: whole steps of 64.
+__device__ __forceinline__ void split_range(int len, int split, int nsplit, int& k0, int& k1) {
+  const int per = ((len + nsplit - 1) / nsplit + 63) & ~63;
+  k0 = __builtin_amdgcn_readfirstlane(min(split * per, len));
+  k1 = __builtin_amdgcn_readfirstlane(min(k0 + per, len));
+}
+
+// ---------------------------------------------------------------------------
+// Fragments.  Scores are computed transposed, S^T (32 tokens x 32 rows) = K . Q^T
+// with mfma 32x32x16, and fed to O^T (32 dims x 32 rows) += V^T . P^T straight
+// from their registers: the tokens are dealt to the first product's rows so that
+// the 16 scores that a lane gets of its query row (lane % 32) are the tokens its
+// half of the wave supplies to the second product.  V blocks are dim-major, so the
+// second product's A operand is a run of tokens of one dim, in one load.
+//   MFMA row m = 8 j + 4 h + e  <->  bf16 pages: token 16 (j / 2) + 8 h + 4 (j % 2) + e
+//   (a lane's registers 8 s .. 8 s + 7: tokens 8 h .. 8 h + 7 of block s)
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ int mfma_token(int m) { return 16 * (m >> 4) + 8 * ((m >> 2) & 1) + 4 * ((m >> 3) & 1) + (m & 3); }
+
+__device__ __forceinline__ bf16x8 ld8(const void* p) { return __builtin_bit_cast(bf16x8, *static_cast<const u32x4*>(p)); }
+
+// Max over the two lanes that share a query row.
+__device__ __forceinline__ float half_max(float v) {
+  const uint32_t x = __float_as_uint(v);
+  const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// One online-softmax step over N scores of a lane's query row (-inf where
+// masked): reference = the row's max, so that a leading token's probability is
+// exactly 1 in bf16; the accumulators are rescaled only when some row's max rose.
+// Scores become probabilities relative to 2^m_run.
+template <int N>
+__device__ __forceinline__ void softmax_step(float (&st)[N], float scale, float& m_run, float& l_run, f32x16 (&o)[4]) {
+  float mx[4] = {st[0], st[1], st[2], st[3]};
+#pragma unroll
+  for (int i = 4; i < N; ++i) mx[i & 3] = fmaxf(mx[i & 3], st[i]);
+  const float bm = half_max(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]))) * scale;
+  const bool rises = bm > m_run;
+  if (__builtin_amdgcn_ballot_w64(rises)) {
+    const float mn = rises ? bm : m_run;
+    const float alpha = rises ? __builtin_amdgcn_exp2f(m_run - mn) : 1.f;
+    l_run *= alpha;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) o[dt] *= alpha;
+    m_run = mn;
+  }
+  const float ms = m_run == -INFINITY ? 0.f : m_run;  // nothing valid yet: exp2(-inf) = 0 all the same
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    st[i] = __builtin_amdgcn_exp2f(fmaf(st[i], scale, -ms));
+    sum[i & 3] += st[i];
+  }
+  l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+}
+
+__device__ __forceinline__ bf16x8 pack8(const float* p) {
+  u32x4 w;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(p[2 * e], p[2 * e + 1]);
+  return __builtin_bit_cast(bf16x8, w);
+}
+
+// Zeroes the tokens from nv on of a V fragment's eight.
+__device__ __forceinline__ bf16x8 keep_tokens(bf16x8 v, int nv) {
+  u32x4 w = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w[e] &= nv >= 2 * e + 2 ? 0xffffffffu : nv == 2 * e + 1 ? 0xffffu : 0u;
+  return __builtin_bit_cast(bf16x8, w);
+}
+__device__ __forceinline__ bool has_nonfinite(bf16x8 v) {
+  const u32x4 w = __builtin_bit_cast(u32x4, v);
+  bool bad = false;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) bad |= (w[e] & 0x7f80u) == 0x7f80u || (w[e] & 0x7f800000u) == 0x7f800000u;
+  return bad;
+}
 
 // Element i of an array of page type PT (e4m3: the code's value, without its scale).
 template <int PT>
@@ -29,72 +246,671 @@ __device__ __forceinline__ float page_at(const void* p, size_t i) {
   if constexpr (PT == kPageE4M3) return __builtin_amdgcn_cvt_f32_fp8((int)static_cast<const uint8_t*>(p)[i], 0);
 }
 
-// One workgroup per (row, head), 256 keys at a time: a thread scores one key,
-// then sums one output dim (any head dim up to 512).
+// One query row over keys k0 .. k1-1 by a workgroup of 256, 256 keys at a time: a
+// thread scores one key, then sums output dims t and t + 256 (any head dim up to
+// 512).  Only keys in the range are touched.  m in the log2 domain; o unnormalised.
 constexpr int kMaxD = 512;
+struct RowLds {
+  float q[kMaxD], p[256], red[4];
+  int id[16];
+};
 template <int PT, typename T>
-__global__ __launch_bounds__(256) void chunk_attn_row_kernel(ChunkAttnK a) {
-  __shared__ float s_q[kMaxD], s_p[256], s_red[4];
-  __shared__ int s_id[16];
-  if (blockIdx.x == 0 && blockIdx.y == 0) chunk_check(a.c);
-  const int row = blockIdx.x, h = blockIdx.y, t = threadIdx.x, D = a.D, g = h / (a.H / a.Hkv);
-  const int b = chunk_find(a.c.B, row, [&](int i) { return a.c.starts[i]; });
-  if (b < 0) return;
-  const ChunkSeq s = chunk_seq(a.c, b);
-  const int i = row - s.s0;
-  if (i >= s.n) return;
-  const T* q = static_cast<const T*>(a.q) + ((size_t)row * a.H + h) * D;
-  for (int d = t; d < D; d += 256) s_q[d] = to_f(q[d]);
-  const int n = s.c + i + 1;
-  float m = -INFINITY, l = 0.f, o[2] = {0.f, 0.f};
+__device__ void attend_row(const ChunkAttnK& a, int b, int g, const T* q, int k0, int k1, RowLds& sh, float& m, float& l,
+                           float (&o)[2]) {
+  const int t = threadIdx.x, D = a.D;
+  __syncthreads();
+  for (int d = t; d < D; d += 256) sh.q[d] = to_f(q[d]);
+  m = -INFINITY;
+  l = o[0] = o[1] = 0.f;
   bool bad = false;
-  for (int k0 = 0; k0 < n; k0 += 256) {
+  for (int b0 = k0; b0 < k1; b0 += 256) {  // k0: a block's first token
     __syncthreads();
     if (t < 16) {
-      const int blk = k0 / kBlock + t;
-      int id = blk * kBlock < n ? a.c.table[(size_t)b * a.c.max_blocks + blk] : 0;
+      const int blk = b0 / kBlock + t;
+      int id = blk * kBlock < k1 ? a.c.table[(size_t)b * a.c.max_blocks + blk] : 0;
       if (id < 0 || id >= a.c.num_blocks) {
         bad = true;
         id = -1;
       }
-      s_id[t] = id;
+      sh.id[t] = id;
     }
     __syncthreads();
-    const int k = k0 + t, id = s_id[t / kBlock];
+    const int k = b0 + t, id = sh.id[t / kBlock];
     float sc = -INFINITY;
-    if (k < n && id >= 0) {
+    if (k < k1 && id >= 0) {
       const size_t slot = ((size_t)id * a.Hkv + g) * kBlock + t % kBlock;
       float dot = 0.f;
-      for (int d = 0; d < D; ++d) dot = fmaf(s_q[d], page_at<PT>(a.kp, slot * D + d), dot);
+      for (int d = 0; d < D; ++d) dot = fmaf(sh.q[d], page_at<PT>(a.kp, slot * D + d), dot);
       if constexpr (PT == kPageE4M3) dot *= __uint_as_float((uint32_t)a.ks[slot] << 23);
       sc = dot * a.scale_log2;
     }
-    const float mn = fmaxf(m, block_max<256>(sc, s_red));
-    const float p = sc == -INFINITY ? 0.f : exp2f(sc - mn), al = m == -INFINITY ? 0.f : exp2f(m - mn);
+    const float mn = fmaxf(m, block_max<256>(sc, sh.red));
+    const float ms = mn == -INFINITY ? 0.f : mn;
+    const float p = exp2f(sc - ms), al = m == -INFINITY ? 0.f : exp2f(m - mn);
     m = mn;
-    l = l * al + block_sum<256>(p, s_red);
-    s_p[t] = p;
+    l = l * al + block_sum<256>(p, sh.red);
+    sh.p[t] = p;
     __syncthreads();
     for (int e = 0; e < 2; ++e) {
       const int d = t + 256 * e;
       if (d >= D) break;
       float acc = o[e] * al;
-      for (int j = 0; j < 256 && k0 + j < n; ++j) {
-        const int jd = s_id[j / kBlock];
+      for (int j = 0; j < 256 && b0 + j < k1; ++j) {
+        const int jd = sh.id[j / kBlock];
         if (jd < 0) continue;
         const size_t head = ((size_t)jd * a.Hkv + g) * kBlock;
         float v = page_at<PT>(a.vp, head * D + (size_t)d * kBlock + j % kBlock);
         if constexpr (PT == kPageE4M3) v *= __uint_as_float((uint32_t)a.vs[head + j % kBlock] << 23);
-        acc = fmaf(s_p[j], v, acc);
+        acc = fmaf(sh.p[j], v, acc);
       }
       o[e] = acc;
     }
   }
   if (bad) flag_error(a.c.err, kErrBlock);
+}
+
+// One workgroup per (row, head).
+template <int PT, typename T>
+__global__ __launch_bounds__(256) void chunk_attn_row_kernel(ChunkAttnK a) {
+  __shared__ RowLds sh;
+  if (blockIdx.x == 0 && blockIdx.y == 0) chunk_check(a.c);
+  const int row = blockIdx.x, h = blockIdx.y, t = threadIdx.x, D = a.D;
+  const int b = chunk_find(a.c.B, row, [&](int i) { return a.c.starts[i]; });
+  if (b < 0) return;
+  const ChunkSeq s = chunk_seq(a.c, b);
+  const int i = row - s.s0;
+  if (i >= s.n) return;
+  float m, l, o[2];
+  const size_t at = ((size_t)row * a.H + h) * D;
+  attend_row<PT, T>(a, b, h / (a.H / a.Hkv), static_cast<const T*>(a.q) + at, 0, s.c + i + 1, sh, m, l, o);
   for (int e = 0; e < 2; ++e) {
     const int d = t + 256 * e;
-    if (d < D) static_cast<T*>(a.out)[((size_t)row * a.H + h) * D + d] = from_f<T>(o[e] / l);
+    if (d < D) static_cast<T*>(a.out)[at + d] = from_f<T>(o[e] / l);
   }
+}
+
+// A piece whose masked tokens hold NaN or infinities in V (a later token of the
+// chunk, seen by some of its rows): in the matrix products 0 times those would
+// reach the rows that do not see them.  The piece's rows again, one at a time, each
+// over the keys that it sees.
+template <int PT, int C>
+__device__ void redo_piece(const ChunkAttnK& a, const Piece& pc, int kvh, int G, int tokens, int k0, int k1, char* lds) {
+  constexpr int ROWS = C == kTiles ? kTileRows : kStreamRows;
+  RowLds& sh = *reinterpret_cast<RowLds*>(lds);
+  const int i0 = pc.tile * tokens, R = min(tokens, pc.s.n - i0) * G;
+  for (int r = 0; r < R; ++r) {
+    const int i = i0 + r / G, row = pc.s.s0 + i;
+    float m, l, o[2];
+    const size_t at = ((size_t)row * a.H + kvh * G + r % G) * kHD;
+    attend_row<PT, bf16_t>(a, pc.b, kvh, static_cast<const bf16_t*>(a.q) + at, k0, min(k1, pc.s.c + i + 1), sh, m, l, o);
+    if (threadIdx.x >= kHD) continue;
+    if (pc.nsplit == 1) {
+      static_cast<bf16_t*>(a.out)[at + threadIdx.x] = f2bf(o[0] / l);
+    } else {
+      const size_t slot = ((size_t)(pc.slot + pc.split) * a.Hkv + kvh) * ROWS + r;
+      a.part_o[C][slot * kHD + threadIdx.x] = o[0];
+      if (threadIdx.x == 0) a.part_ml[C][slot] = float2{m, l};
+    }
+  }
+}
+
+// A lane's row of a piece: 4 consecutive dims per register quad.
+__device__ __forceinline__ void store_row(const ChunkAttnK& a, int row, int head, const f32x16 (&o)[4], float inv) {
+  bf16_t* dst = static_cast<bf16_t*>(a.out) + ((size_t)row * a.H + head) * kHD + 4 * ((threadIdx.x & 63) >> 5);
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *reinterpret_cast<u32x2*>(dst + 32 * dt + 8 * j) =
+          u32x2{pack_bf16x2(o[dt][4 * j] * inv, o[dt][4 * j + 1] * inv),
+                pack_bf16x2(o[dt][4 * j + 2] * inv, o[dt][4 * j + 3] * inv)};
+}
+
+// ---------------------------------------------------------------------------
+// Tiles: 128 query rows per workgroup, 32 per wave; keys and values pass through
+// LDS 64 tokens (four blocks) at a time, two buffers.  LDS holds bf16 whatever the
+// pages hold: bf16 pages are copied by the load itself (global_load_lds_dwordx4),
+// e4m3 ones are converted once per workgroup on the way (exact: a code times a
+// power of two).
+//
+// Bound by the matrix cores and the softmax's vector work about alike: 64 tokens
+// take a wave 32 MFMAs of 32 clocks and ~200 vector instructions.
+//
+// Swizzle, in 16-byte units: K token t of a block keeps unit u at u ^ t; V dim d
+// keeps its two halves swapped when bit 4 of d is set.  The 16 lanes that a
+// fragment read serves together (0-3, 12-15, 20-27; 4-11, 16-19, 28-31; the same
+// from 32 on) then hit 16 different units of the 256 bytes of banks.
+// ---------------------------------------------------------------------------
+constexpr int kStep = 64;                        // tokens per stage
+constexpr int kStageBytes = kStep * kHD * 2 * 2; // K of four blocks, then V of them
+constexpr int kBlkBytes = kBlock * kHD * 2;
+template <int PT>
+__global__ __launch_bounds__(256, 2) void chunk_tile_kernel(ChunkAttnK a) {
+  __shared__ __attribute__((aligned(1024))) char smem[2 * kStageBytes];
+  const int kvh = __builtin_amdgcn_readfirstlane(blockIdx.x % a.Hkv);
+  if (blockIdx.x == 0) chunk_check(a.c);
+  Piece pc;
+  if (!find_piece<kTiles>(a, blockIdx.x / a.Hkv, false, pc)) return;
+  const int G = __builtin_amdgcn_readfirstlane(a.H / a.Hkv), tokens = __builtin_amdgcn_readfirstlane(kTileRows / G);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r32 = lane & 31, h = lane >> 5;
+  const int i0 = pc.tile * tokens, len = pc.s.c + min(i0 + tokens, pc.s.n);
+  int k0, k1;
+  split_range(len, pc.split, pc.nsplit, k0, k1);
+
+  // this lane's query row, its last visible key, and the wave's first and last
+  const int r = wave * 32 + r32, i = i0 + r / G, head = kvh * G + r % G;
+  const bool row_ok = r < tokens * G && i < pc.s.n;
+  const int ic = min(i, pc.s.n - 1), vis = pc.s.c + ic;
+  const int row = pc.s.s0 + ic;
+  const int vis_lo = pc.s.c + __builtin_amdgcn_readfirstlane(min(i0 + wave * 32 / G, pc.s.n - 1));
+  const int vis_hi = pc.s.c + __builtin_amdgcn_readfirstlane(min(i0 + (wave * 32 + 31) / G, pc.s.n - 1));
+  const bool wave_on = wave * 32 < tokens * G && i0 + wave * 32 / G < pc.s.n;
+  bf16x8 qf[8];
+  {
+    const bf16_t* src = static_cast<const bf16_t*>(a.q) + ((size_t)row * a.H + min(head, a.H - 1)) * kHD + 8 * h;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) qf[s] = ld8(src + 16 * s);
+  }
+  float m_run = -INFINITY, l_run = 0.f;
+  f32x16 o[4];
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[dt][e] = 0.f;
+
+  bool odd = false;  // see redo_piece
+  const int nit = (k1 - k0 + kStep - 1) / kStep;
+  // page ids of this wave's block of 64 stages (lane l: stage idbase + l); bad
+  // ones and blocks behind the last key read page 0, whose tokens are masked (or,
+  // for a bad id, make the output undefined)
+  int idv = 0, idbase = 0;
+  bool bad = false;
+  auto read_ids = [&](int it0) {
+    idbase = it0;
+    const int blk = (k0 + (it0 + lane) * kStep) / kBlock + wave;
+    int id = 0;
+    if (blk * kBlock < k1) {
+      id = a.c.table[(size_t)pc.b * a.c.max_blocks + blk];
+      if (id < 0 || id >= a.c.num_blocks) {
+        bad = true;
+        id = 0;
+      }
+    }
+    idv = id;
+  };
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+  // bf16: source offsets of the four 1 KB pieces of a K block (its rows 4 q ..) and of a V block
+  uint32_t kofs[4], vofs[4];
+  if constexpr (PT == kPageBF16) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int p = q * 64 + lane, t = p >> 4, d = p >> 1;
+      kofs[q] = (uint32_t)(t * kHD * 2 + (((p & 15) ^ t) * 16));
+      vofs[q] = (uint32_t)(d * kBlock * 2 + (((p & 1) ^ ((d >> 4) & 1)) * 16));
+    }
+  }
+  // e4m3: a block's K and V codes, two 16-byte pieces a lane, and their scales
+  u32x4 kc[2], vc[2], vsc;
+  uint32_t ksc[2];
+  auto load = [&](int it) {
+    if (it - idbase >= 64) read_ids(it);
+    const int id = __builtin_amdgcn_readlane(idv, it - idbase);
+    const size_t hd = (size_t)id * a.Hkv + kvh;
+    if constexpr (PT == kPageBF16) {
+      const char* ksrc = static_cast<const char*>(a.kp) + hd * kBlkBytes;
+      const char* vsrc = static_cast<const char*>(a.vp) + hd * kBlkBytes;
+      const uint32_t dst = lds0 + (it & 1) * kStageBytes + wave * kBlkBytes;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(kofs[q]), "s"(ksrc), "s"(dst + q * 1024) : "memory", "m0");
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(vofs[q]), "s"(vsrc), "s"(dst + kStageBytes / 2 + q * 1024) : "memory", "m0");
+    } else {
+      const char* ksrc = static_cast<const char*>(a.kp) + hd * (kBlkBytes / 2);
+      const char* vsrc = static_cast<const char*>(a.vp) + hd * (kBlkBytes / 2);
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        kc[q] = *reinterpret_cast<const u32x4*>(ksrc + (q * 64 + lane) * 16);
+        vc[q] = *reinterpret_cast<const u32x4*>(vsrc + (q * 64 + lane) * 16);
+        ksc[q] = a.ks[hd * kBlock + q * 8 + (lane >> 3)];
+      }
+      vsc = *reinterpret_cast<const u32x4*>(a.vs + hd * kBlock);
+    }
+  };
+  auto convert = [&](int it) {
+    if constexpr (PT == kPageE4M3) {
+      char* kd = smem + (it & 1) * kStageBytes + wave * kBlkBytes;
+      char* vd = kd + kStageBytes / 2;
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int p = q * 64 + lane, t = p >> 3, u = 2 * (p & 7);
+        u32x4 w[2];
+        const float sc = __uint_as_float(ksc[q] << 23);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)kc[q][c], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)kc[q][c], true);
+          w[c >> 1][2 * (c & 1)] = pack_bf16x2(lo[0] * sc, lo[1] * sc);
+          w[c >> 1][2 * (c & 1) + 1] = pack_bf16x2(hi[0] * sc, hi[1] * sc);
+        }
+        *reinterpret_cast<u32x4*>(kd + t * 256 + ((u ^ t) * 16)) = w[0];
+        *reinterpret_cast<u32x4*>(kd + t * 256 + (((u + 1) ^ t) * 16)) = w[1];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)vc[q][c], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)vc[q][c], true);
+          auto vscale = [&](int e) { return __uint_as_float(((vsc[c] >> (8 * e)) & 0xffu) << 23); };
+          w[c >> 1][2 * (c & 1)] = pack_bf16x2(lo[0] * vscale(0), lo[1] * vscale(1));
+          w[c >> 1][2 * (c & 1) + 1] = pack_bf16x2(hi[0] * vscale(2), hi[1] * vscale(3));
+        }
+        const int swap = (p >> 4) & 1;
+        *reinterpret_cast<u32x4*>(vd + p * 32 + (0 ^ swap) * 16) = w[0];
+        *reinterpret_cast<u32x4*>(vd + p * 32 + (1 ^ swap) * 16) = w[1];
+      }
+    }
+  };
+  // fragment addresses: K row of MFMA row r32, V dim r32
+  const int mt = mfma_token(r32);
+  const int kaddr = (mt >> 4) * kBlkBytes + (mt & 15) * 256 + ((h ^ (mt & 15)) * 16);
+  const int vaddr = kStageBytes / 2 + r32 * 32 + ((h ^ (r32 >> 4)) * 16);
+
+  if (nit > 0) {
+    read_ids(0);
+    load(0);
+    convert(0);
+  }
+  for (int it = 0; it < nit; ++it) {
+    // this stage is in LDS (loads of the compiler's own are waited for with it), and every wave is done with the
+    // buffer that the next one goes to
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (it + 1 < nit) load(it + 1);
+    const char* buf = smem + (it & 1) * kStageBytes;
+    const int t0 = k0 + it * kStep;
+    if (wave_on && t0 <= vis_hi) {
+      f32x16 acc[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[x][e] = 0.f;
+#pragma unroll
+        for (int s = 0; s < 8; ++s)
+          acc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld8(buf + ((kaddr ^ (32 * s)) + x * 2 * kBlkBytes)), qf[s], acc[x], 0, 0, 0);
+      }
+      float st[32];
+#pragma unroll
+      for (int e = 0; e < 32; ++e) st[e] = acc[e >> 4][e & 15];
+      const bool masked = t0 + kStep - 1 > vis_lo || t0 + kStep > k1;
+      const int lim = min(vis, k1 - 1) - t0;
+      if (masked) {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) st[e] = 16 * (e >> 3) + 8 * h + (e & 7) <= lim ? st[e] : -INFINITY;
+      }
+      softmax_step(st, a.scale_log2, m_run, l_run, o);
+      if (masked) {  // a masked token's V must not be NaN or infinite: 0 times it would not be 0
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+          for (int dt = 0; dt < 4; ++dt)
+            odd |= has_nonfinite(keep_tokens(ld8(buf + vaddr + x * kBlkBytes + dt * 1024), k1 - t0 - 16 * x - 8 * h));
+      }
+      const bool tail = t0 + kStep > k1;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const bf16x8 pf = pack8(st + 8 * x);
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) {
+          bf16x8 vf = ld8(buf + vaddr + x * kBlkBytes + dt * 1024);
+          if (tail) vf = keep_tokens(vf, k1 - t0 - 16 * x - 8 * h);
+          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[dt], 0, 0, 0);
+        }
+      }
+    }
+    if (it + 1 < nit) convert(it + 1);
+  }
+  if (__builtin_amdgcn_ballot_w64(bad) && lane == 0) flag_error(a.c.err, kErrBlock);
+  if (__syncthreads_or(odd)) {
+    redo_piece<PT, kTiles>(a, pc, kvh, G, tokens, k0, k1, smem);
+    return;
+  }
+  const float l = l_run + __shfl_xor(l_run, 32);
+  if (pc.nsplit == 1) {
+    if (row_ok) store_row(a, row, head, o, 1.0f / l);
+    return;
+  }
+  if (!row_ok) return;
+  const size_t slot = ((size_t)(pc.slot + pc.split) * a.Hkv + kvh) * kTileRows + r;
+  float* dst = a.part_o[kTiles] + slot * kHD + 4 * h;
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *reinterpret_cast<f32x4*>(dst + 32 * dt + 8 * j) = f32x4{o[dt][4 * j], o[dt][4 * j + 1], o[dt][4 * j + 2], o[dt][4 * j + 3]};
+  if (h == 0) a.part_ml[kTiles][slot] = float2{m_run, l};
+}
+
+// ---------------------------------------------------------------------------
+// Streamed: up to 16 RT query rows (decoding steps and short chunks), RT = 1 or 2
+// row tiles.  Each wave takes steps of its own (step w, w + 4, .. of the piece)
+// straight from memory into MFMA fragments, and the four waves' results are joined
+// in LDS.  Bound by the read of the cache; what is in flight (16 KB a wave) sets
+// the rate.
+//
+// A step is 32 tokens in bf16 and 64 in e4m3: every load is then 16 bytes a lane,
+// 16 KB a step.  W = 8 or 16 tokens per lane group g = lane / 16: row m of score
+// tile j (mfma 16x16x32) is token W (m / 4) + 4 j + m % 4, so that group g ends up
+// with the scores of tokens W g .. in order, the very run of a dim of a V block that
+// the group's loads bring for the second product.  e4m3: 16 codes of K are two
+// k-steps of the first product (q's fragments are dealt the same way) and take the
+// token's scale as they are converted; V's scales multiply the probabilities.
+// ---------------------------------------------------------------------------
+// Eight e4m3 codes as bf16, times a power of two (exact).
+__device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t c0, uint32_t c1, float sc) {
+  u32x4 w;
+  w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)c0, sc, false));
+  w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)c0, sc, true));
+  w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)c1, sc, false));
+  w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)c1, sc, true));
+  return __builtin_bit_cast(bf16x8, w);
+}
+
+// Max over the four lanes that share a query row (lane % 16).
+__device__ __forceinline__ float quarter_max(float v) {
+  const uint32_t x = __float_as_uint(v);
+  const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  return half_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+
+constexpr int kMergeRow = kHD + 4;  // LDS row stride of the wave merge, in floats
+template <int PT, int RT>
+__global__ __launch_bounds__(256, 2) void chunk_stream_kernel(ChunkAttnK a) {
+  constexpr bool E4 = PT == kPageE4M3;
+  constexpr int NP = 4, ROWS = 16 * RT;
+  constexpr int W = E4 ? 16 : 8, ST = 4 * W, NT = W / 4;  // tokens of a lane group and of a step, score tiles
+  __shared__ __attribute__((aligned(16))) float s_o[NP][ROWS * kMergeRow];
+  __shared__ float s_m[NP][ROWS], s_l[NP][ROWS];
+  const int kvh = __builtin_amdgcn_readfirstlane(blockIdx.x % a.Hkv);
+  if (blockIdx.x == 0) chunk_check(a.c);
+  Piece pc;
+  if (!find_piece<kStream>(a, blockIdx.x / a.Hkv, false, pc)) return;
+  const int G = __builtin_amdgcn_readfirstlane(a.H / a.Hkv), R = pc.s.n * G, len = pc.s.c + pc.s.n;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r16 = lane & 15, g = lane >> 4;
+  int k0, k1;
+  split_range(len, pc.split, pc.nsplit, k0, k1);
+  const int np = (k1 - k0 + ST - 1) / ST;                   // steps of the piece
+  const int n = np > wave ? (np - wave + NP - 1) / NP : 0;  // this wave's
+
+  bf16x8 qf[RT][4];
+  int vis[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int qr = min(16 * t + r16, R - 1), qi = qr / G;  // padding rows repeat the last one
+    const bf16_t* src = static_cast<const bf16_t*>(a.q) + ((size_t)(pc.s.s0 + qi) * a.H + kvh * G + qr % G) * kHD;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) qf[t][s] = ld8(src + (E4 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g));
+    vis[t] = pc.s.c + qi;
+  }
+  // page ids of 64 / NT of the wave's steps: lane l holds block l % NT of step
+  // idbase + l / NT; -1 behind the last key (its tokens are masked) and for a bad
+  // id (the output is then undefined): both read page 0
+  constexpr int kIds = kWave / NT;
+  int idv = -1, idbase = 0;
+  bool bad = false;
+  auto read_ids = [&](int j0) {
+    idbase = j0;
+    const int blk = k0 / kBlock + NT * (wave + NP * (j0 + lane / NT)) + lane % NT;
+    int id = -1;
+    if (blk * kBlock < k1) {
+      id = a.c.table[(size_t)pc.b * a.c.max_blocks + blk];
+      if (id < 0 || id >= a.c.num_blocks) {
+        bad = true;
+        id = -1;
+      }
+    }
+    idv = id;
+  };
+  read_ids(0);
+  bool odd = false;  // see redo_piece
+  u32x4 kr[8], vr[8], vsc;
+  uint32_t ksc[NT];
+  int ids[NT];  // pages of the step whose K is loaded
+  // this lane's page of the step: of the token that it holds for K (block (W / 16 ..) of row m) and for V
+  auto pick = [&](int blk) {
+    int id = ids[0];
+#pragma unroll
+    for (int i = 1; i < NT; ++i) id = blk == i ? ids[i] : id;
+    return (size_t)max(id, 0) * a.Hkv + kvh;
+  };
+  const int ktok = W * (r16 >> 2) + (r16 & 3);  // token of score tile 0 (tile j: + 4 j, in the same block)
+  auto load_k = [&](int j) {
+    if (j - idbase >= kIds) read_ids(j);
+#pragma unroll
+    for (int i = 0; i < NT; ++i) ids[i] = __builtin_amdgcn_readlane(idv, NT * (j - idbase) + i);
+    const size_t hd = pick(ktok >> 4);
+    if constexpr (E4) {
+      const char* src = static_cast<const char*>(a.kp) + (hd * kBlock + (ktok & 15)) * kHD + 16 * g;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) kr[2 * t + s] = *reinterpret_cast<const u32x4*>(src + 4 * t * kHD + 64 * s);
+        ksc[t] = a.ks[hd * kBlock + (ktok & 15) + 4 * t];
+      }
+    } else {
+      const char* src = static_cast<const char*>(a.kp) + ((hd * kBlock + (ktok & 15)) * kHD + 8 * g) * 2;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int s = 0; s < 4; ++s) kr[4 * t + s] = *reinterpret_cast<const u32x4*>(src + 4 * t * kHD * 2 + 64 * s);
+    }
+  };
+  auto load_v = [&]() {
+    const size_t hd = pick(W * g >> 4);
+    const char* src = static_cast<const char*>(a.vp) +
+                      (E4 ? (hd * kHD + r16) * kBlock : ((hd * kHD + r16) * kBlock + 8 * (g & 1)) * 2);
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) vr[dt] = *reinterpret_cast<const u32x4*>(src + dt * 16 * kBlock * (E4 ? 1 : 2));
+    if constexpr (E4) vsc = *reinterpret_cast<const u32x4*>(a.vs + hd * kBlock);
+  };
+  float m_run[RT], l_run[RT];
+  f32x4 o[RT][8];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    m_run[t] = -INFINITY;
+    l_run[t] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) o[t][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  if (n > 0) {
+    load_k(0);
+    load_v();
+  }
+  for (int j = 0; j < n; ++j) {
+    f32x4 acc[RT][NT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int i = 0; i < NT; ++i) acc[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      const float sc = E4 ? __uint_as_float(ksc[i] << 23) : 1.f;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        bf16x8 kf;
+        if constexpr (E4) {
+          const u32x4 c = kr[2 * i + (s >> 1)];
+          kf = codes_to_bf16(c[2 * (s & 1)], c[2 * (s & 1) + 1], sc);
+        } else {
+          kf = __builtin_bit_cast(bf16x8, kr[4 * i + s]);
+        }
+#pragma unroll
+        for (int t = 0; t < RT; ++t) acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][s], acc[t][i], 0, 0, 0);
+      }
+      if constexpr (E4) __builtin_amdgcn_sched_barrier(0);  // conversions hoisted further would need registers of their own
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (j + 1 < n) load_k(j + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    const int t0 = k0 + ST * (wave + NP * j);
+    const bool masked = t0 + ST - 1 > pc.s.c || t0 + ST > k1;
+    float st[RT][W];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+#pragma unroll
+      for (int e = 0; e < W; ++e) st[t][e] = acc[t][e >> 2][e & 3];
+      if (masked) {
+        const int lim = min(vis[t], k1 - 1) - t0 - W * g;
+#pragma unroll
+        for (int e = 0; e < W; ++e) st[t][e] = e <= lim ? st[t][e] : -INFINITY;
+      }
+      // online softmax, reference = the row's max (see softmax_step)
+      float mx[4] = {st[t][0], st[t][1], st[t][2], st[t][3]};
+#pragma unroll
+      for (int e = 4; e < W; ++e) mx[e & 3] = fmaxf(mx[e & 3], st[t][e]);
+      const float bm = quarter_max(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]))) * a.scale_log2;
+      const bool rises = bm > m_run[t];
+      if (__builtin_amdgcn_ballot_w64(rises)) {
+        const float mn = rises ? bm : m_run[t];
+        const float alpha = rises ? __builtin_amdgcn_exp2f(m_run[t] - mn) : 1.f;
+        l_run[t] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) o[t][dt] *= alpha;
+        m_run[t] = mn;
+      }
+      const float ms = m_run[t] == -INFINITY ? 0.f : m_run[t];
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < W; ++e) {
+        st[t][e] = __builtin_amdgcn_exp2f(fmaf(st[t][e], a.scale_log2, -ms));
+        sum[e & 3] += st[t][e];
+      }
+      l_run[t] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    }
+    if (masked) {  // a masked token's V must not be NaN or infinite: 0 times it would not be 0
+      const int nv = k1 - t0 - W * g;  // tokens of the lane's run before the end: the others may be anything, and are zeroed
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) {
+        if constexpr (E4) {
+          uint32_t any = 0;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const int k = min(max(nv - 4 * c, 0), 4);
+            vr[dt][c] &= k == 4 ? 0xffffffffu : (1u << (8 * k)) - 1u;
+            any |= (vr[dt][c] & 0x7f7f7f7fu) + 0x01010101u;  // a NaN code (magnitude 0x7f) carries into its top bit
+          }
+          odd |= (any & 0x80808080u) != 0;
+        } else {
+          const bf16x8 v = keep_tokens(__builtin_bit_cast(bf16x8, vr[dt]), nv);
+          vr[dt] = __builtin_bit_cast(u32x4, v);
+          odd |= has_nonfinite(v);
+        }
+      }
+    }
+    {
+#pragma unroll
+      for (int t = 0; t < RT; ++t)
+        if constexpr (E4) {
+#pragma unroll
+          for (int e = 0; e < W; ++e) {
+            // (a masked token's slot may hold any scale byte: its probability stays 0)
+            const float sc = __uint_as_float(((vsc[e >> 2] >> (8 * (e & 3))) & 0xffu) << 23);
+            st[t][e] = st[t][e] == 0.f ? 0.f : st[t][e] * sc;
+          }
+        }
+#pragma unroll
+      for (int x = 0; x < W / 8; ++x) {
+        bf16x8 pf[RT];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) pf[t] = pack8(&st[t][8 * x]);
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) {
+          bf16x8 vf;  // k-step x (tokens W g + 8 x ..) of dims 16 dt ..
+          if constexpr (E4)
+            vf = codes_to_bf16(vr[dt][2 * x], vr[dt][2 * x + 1], 1.f);
+          else
+            vf = __builtin_bit_cast(bf16x8, vr[dt]);
+#pragma unroll
+          for (int t = 0; t < RT; ++t) o[t][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[t], o[t][dt], 0, 0, 0);
+          if constexpr (E4)
+            if (dt % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (j + 1 < n) load_v();
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  if (__builtin_amdgcn_ballot_w64(bad) && lane == 0) flag_error(a.c.err, kErrBlock);
+
+  if (__syncthreads_or(odd)) {
+    redo_piece<PT, kStream>(a, pc, kvh, G, pc.s.n, k0, k1, reinterpret_cast<char*>(s_o));
+    return;
+  }
+  // join the waves, then store the rows or this split's part
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    float l = l_run[t];
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (g == 0) {
+      s_m[wave][16 * t + r16] = m_run[t];
+      s_l[wave][16 * t + r16] = l;
+    }
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt)
+      *reinterpret_cast<f32x4*>(&s_o[wave][(16 * t + r16) * kMergeRow + 16 * dt + 4 * g]) = o[t][dt];
+  }
+  __syncthreads();
+  for (int u = threadIdx.x; u < R * (kHD / 4); u += 256) {
+    const int rr = u / (kHD / 4), d = (u % (kHD / 4)) * 4;
+    float mx = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < NP; ++w) mx = fmaxf(mx, s_m[w][rr]);
+    f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < NP; ++w) {
+      const float m = s_m[w][rr], f = m == -INFINITY ? 0.f : exp2f(m - mx);
+      sum += f * s_l[w][rr];
+      acc += f * *reinterpret_cast<const f32x4*>(&s_o[w][rr * kMergeRow + d]);
+    }
+    if (pc.nsplit == 1) {
+      const float inv = 1.0f / sum;
+      bf16_t* dst = static_cast<bf16_t*>(a.out) + ((size_t)(pc.s.s0 + rr / G) * a.H + kvh * G + rr % G) * kHD + d;
+      *reinterpret_cast<u32x2*>(dst) = u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
+    } else {
+      const size_t slot = ((size_t)(pc.slot + pc.split) * a.Hkv + kvh) * kStreamRows + rr;
+      *reinterpret_cast<f32x4*>(a.part_o[kStream] + slot * kHD + d) = acc;
+      if (d == 0) a.part_ml[kStream][slot] = float2{mx, sum};
+    }
+  }
+}
+
+// Joins the parts of pieces whose keys were cut:
+//   out = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s.
+// grid (split tiles of the class per KV head * Hkv, row groups of 8); 4 dims of a row per thread.
+template <int C>
+__global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkAttnK a) {
+  constexpr int ROWS = C == kTiles ? kTileRows : kStreamRows;
+  const int kvh = __builtin_amdgcn_readfirstlane(blockIdx.x % a.Hkv);
+  Piece pc;
+  if (!find_piece<C>(a, blockIdx.x / a.Hkv, true, pc)) return;
+  const int G = a.H / a.Hkv, tokens = C == kTiles ? kTileRows / G : pc.s.n;
+  const int r = blockIdx.y * 8 + threadIdx.x / (kHD / 4), d = (threadIdx.x % (kHD / 4)) * 4, i = pc.tile * tokens + r / G;
+  if (r >= tokens * G || i >= pc.s.n) return;
+  const size_t base = ((size_t)pc.slot * a.Hkv + kvh) * ROWS + r, step = (size_t)a.Hkv * ROWS;
+  float mx = -INFINITY;
+  for (int s = 0; s < pc.nsplit; ++s) mx = fmaxf(mx, a.part_ml[C][base + s * step].x);
+  f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+  float sum = 0.f;
+  for (int s = 0; s < pc.nsplit; ++s) {
+    const float2 ml = a.part_ml[C][base + s * step];
+    const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - mx);
+    sum += f * ml.y;
+    acc += f * *reinterpret_cast<const f32x4*>(a.part_o[C] + (base + s * step) * kHD + d);
+  }
+  const float inv = 1.0f / sum;
+  bf16_t* dst = static_cast<bf16_t*>(a.out) + ((size_t)(pc.s.s0 + i) * a.H + kvh * G + r % G) * kHD + d;
+  *reinterpret_cast<u32x2*>(dst) = u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
 }
 
 }  // namespace
@@ -155,6 +971,72 @@ int page_type(const nj_kv_layer* kv) { return kv->dtype == NJ_F32 ? kPageF32 : k
 
 constexpr size_t kErrBytes = 256;
 
+// Workspace of the attention: [error word][parts of the tiles][parts of the streamed pieces].
+struct AttnParts {
+  bool tiles, stream;
+  size_t o[2], ml[2], total;
+};
+AttnParts attn_parts(const nj_model_desc& d, int max_chunk) {
+  AttnParts p{};
+  p.total = kErrBytes;
+  const int G = d.n_heads / d.n_kv_heads;
+  if (d.dtype == NJ_F32 || G > kTileRows) return p;
+  p.tiles = (int64_t)max_chunk * G > kStreamRows;
+  p.stream = G <= (p.tiles ? 16 : kStreamRows);
+  const int rows[2] = {kTileRows, kStreamRows};
+  const bool used[2] = {p.tiles, p.stream};
+  for (int c = 0; c < 2; ++c)
+    if (used[c]) {
+      p.o[c] = p.total;
+      p.ml[c] = p.o[c] + (size_t)kSlots[c] * rows[c] * kHD * 4;
+      p.total = p.ml[c] + (size_t)kSlots[c] * rows[c] * 8;
+    }
+  return p;
+}
+
+// Which kernels a batch needs.  Batches of short chunks (up to 32 query rows per
+// KV head, two of the stream kernel's row tiles) are streamed; where longer ones are
+// about, sequences of up to 16 rows are streamed and the others go by tiles.  Where
+// the batch can hold no short sequence (or only by padding), the tiles take
+// everything, and one launch is saved.
+hipError_t launch_chunk_attn(ChunkAttnK& a, const AttnParts& p, int pt, int B, int rows, int max_chunk, hipStream_t s) {
+  const int G = a.H / a.Hkv;
+  if (pt == kPageF32 || G > kTileRows) {
+    auto kern = pt == kPageF32    ? chunk_attn_row_kernel<kPageF32, float>
+                : pt == kPageBF16 ? chunk_attn_row_kernel<kPageBF16, bf16_t>
+                                  : chunk_attn_row_kernel<kPageE4M3, bf16_t>;
+    hipLaunchKernelGGL(kern, dim3(rows, a.H), dim3(256), 0, s, a);
+    return hipGetLastError();
+  }
+  const bool all_long = p.tiles && (!p.stream || (int64_t)B * max_chunk <= rows);
+  const bool one_tile = p.tiles || max_chunk * G <= 16;  // of the stream kernel's 16-row tiles
+  a.threshold = all_long ? 0 : p.tiles ? 16 : INT_MAX;
+  hipError_t e = hipSuccess;
+  if (p.tiles) {
+    const int tokens = kTileRows / G, pieces = std::max(rows / tokens + std::min(B, rows), kSlots[kTiles] / a.Hkv);
+    hipLaunchKernelGGL(pt == kPageE4M3 ? chunk_tile_kernel<kPageE4M3> : chunk_tile_kernel<kPageBF16>, dim3(pieces * a.Hkv),
+                       dim3(256), 0, s, a);
+    e = hipGetLastError();
+    if (e == hipSuccess && kSlots[kTiles] / a.Hkv >= 2) {
+      hipLaunchKernelGGL(chunk_merge_kernel<kTiles>, dim3(kSlots[kTiles] / a.Hkv / 2 * a.Hkv, kTileRows / 8), dim3(256), 0, s, a);
+      e = hipGetLastError();
+    }
+  }
+  if (!all_long && e == hipSuccess) {
+    const int pieces = std::max(std::min(B, rows), kSlots[kStream] / a.Hkv);
+    auto kern = pt == kPageE4M3 ? (one_tile ? chunk_stream_kernel<kPageE4M3, 1> : chunk_stream_kernel<kPageE4M3, 2>)
+                                : (one_tile ? chunk_stream_kernel<kPageBF16, 1> : chunk_stream_kernel<kPageBF16, 2>);
+    hipLaunchKernelGGL(kern, dim3(pieces * a.Hkv), dim3(256), 0, s, a);
+    e = hipGetLastError();
+    const int split = std::min(std::min(B, rows), kSlots[kStream] / a.Hkv / 2);
+    if (e == hipSuccess && split > 0) {
+      hipLaunchKernelGGL(chunk_merge_kernel<kStream>, dim3(split * a.Hkv, kStreamRows / 8), dim3(256), 0, s, a);
+      e = hipGetLastError();
+    }
+  }
+  return e;
+}
+
 }  // namespace
 
 extern "C" {
@@ -192,7 +1074,7 @@ int nightjar_chunk_load(const nj_model_desc* desc, const nj_kv_layer* kv, const 
 
 size_t nightjar_chunk_attn_workspace_bytes(const nj_model_desc* desc, int32_t B, int32_t rows, int32_t max_chunk) {
   if (!chunk_sizes(desc, "chunk_attn") || !batch_sizes("chunk_attn", B, rows, max_chunk)) return 0;
-  return kErrBytes;
+  return attn_parts(*desc, max_chunk).total;
 }
 
 int nightjar_chunk_attn(const nj_model_desc* desc, const nj_kv_layer* kv, const nj_chunk_batch* batch, const void* q,
@@ -208,14 +1090,24 @@ int nightjar_chunk_attn(const nj_model_desc* desc, const nj_kv_layer* kv, const 
   const size_t row_bytes = (size_t)batch->rows * d.n_heads * d.head_dim * (d.dtype == NJ_F32 ? 4 : 2);
   if ((uintptr_t)q < (uintptr_t)out + row_bytes && (uintptr_t)out < (uintptr_t)q + row_bytes)
     return set_last_error(NJ_EINVAL, "chunk_attn: q and out overlap");
-  ChunkAttnK a{c, q, kv->k, kv->v, static_cast<const uint8_t*>(kv->k_scale), static_cast<const uint8_t*>(kv->v_scale),
-               out, d.n_heads, d.n_kv_heads, d.head_dim, 1.4426950408889634f / sqrtf((float)d.head_dim)};
-  const int pt = page_type(kv);
-  auto kern = pt == kPageF32    ? chunk_attn_row_kernel<kPageF32, float>
-              : pt == kPageBF16 ? chunk_attn_row_kernel<kPageBF16, bf16_t>
-                                : chunk_attn_row_kernel<kPageE4M3, bf16_t>;
-  hipLaunchKernelGGL(kern, dim3(batch->rows, d.n_heads), dim3(256), 0, (hipStream_t)stream, a);
-  const hipError_t e = hipGetLastError();
+  const AttnParts p = attn_parts(d, batch->max_chunk);
+  ChunkAttnK a{};
+  a.c = c;
+  a.q = q;
+  a.kp = kv->k;
+  a.vp = kv->v;
+  a.ks = static_cast<const uint8_t*>(kv->k_scale);
+  a.vs = static_cast<const uint8_t*>(kv->v_scale);
+  a.out = out;
+  a.H = d.n_heads;
+  a.Hkv = d.n_kv_heads;
+  a.D = d.head_dim;
+  a.scale_log2 = 1.4426950408889634f / sqrtf((float)d.head_dim);
+  for (int k = 0; k < 2; ++k) {
+    a.part_o[k] = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.o[k]);
+    a.part_ml[k] = reinterpret_cast<float2*>(static_cast<char*>(workspace) + p.ml[k]);
+  }
+  const hipError_t e = launch_chunk_attn(a, p, page_type(kv), batch->B, batch->rows, batch->max_chunk, (hipStream_t)stream);
   return e == hipSuccess ? NJ_OK : set_last_error(NJ_EHIP, "chunk_attn: %s", hipGetErrorString(e));
 }
 

@@ -325,3 +325,53 @@ def test_graph_replay_and_other_stream():
         go()
     side.synchronize()
     assert torch.equal(out, want) and c.error() == 0
+
+
+@pytest.mark.parametrize("pages,shape", [("e4m3", L8), ("bf16", L8), ("bf16", L7), ("f32", TF)], ids=["e4m3-8b", "bf16-8b", "bf16-7b", "f32-tiny"])
+@pytest.mark.parametrize("n,at", [(3, 1), (6, 4), (40, 0), (40, 33), (130, 128)])
+@pytest.mark.parametrize("what", ["v", "k"])
+def test_nonfinite_tokens_reach_only_rows_that_see_them(pages, shape, n, at, what):
+    """Token `at` of the chunk holds NaN (or, where the pages can, infinities): the rows before it are as without it."""
+    c = Case(shape, pages, [n, 2], [150, 20], seed=n)
+    vals = c.fill_context()
+    pos = 150 + at
+    blk, slot = int(c.table[0, pos // 16]), pos % 16
+    t = c.k[blk, :, slot] if what == "k" else c.v[blk, :, :, slot]
+    if pages == "e4m3":
+        t[:] = 0x7F
+    else:
+        t[:, ::2], t[:, 1::2] = float("nan"), float("inf")
+    q = torch.as_tensor(c.rng.normal(size=(c.rows, shape.n_heads, shape.head_dim))).to("cuda", c.rdt)
+    out = torch.full((c.rows, shape.n_heads * shape.head_dim), -7.0, dtype=c.rdt, device="cuda")
+    chunk_attn(c.desc, c.layer, c.batch, q, out, c.ws)
+    assert c.error() == 0
+    seen = out[at:n].float()
+    assert not torch.isfinite(seen).any() if what == "v" else torch.isnan(seen).all()
+    out[at:n] = 0
+    keep = np.r_[0:at, n:n + 2]
+    half, D = (2.0 ** -8 if c.rdt == torch.bfloat16 else 0.0), shape.head_dim
+    got = out.double().cpu().numpy().reshape(c.rows, shape.n_heads, D)
+    qd = q.double().cpu().numpy()
+    k, v = (x[:pos] for x in vals[0])
+    for r0, r1, (kk, vv), ctx in ((0, at, (k, v), 150), (n, n + 2, vals[1], 20)):
+        if r1 > r0:
+            o, a, big = ref.attention(qd[r0:r1], kk, vv, ctx)
+            tol = 1.02 * (half * (a + np.abs(o)) + (2 * (D + 2) * 2.0 ** -24 * big + 200 * 2.0 ** -24) * a) + 2.0 ** -23 * np.abs(o)
+            assert (np.abs(got[r0:r1] - o) <= tol).all()
+    assert np.isfinite(got[keep]).all()
+
+
+@pytest.mark.parametrize("pages", ["bf16", "e4m3"])
+@pytest.mark.parametrize("n", [1, 100])
+def test_attention_of_padded_batches(pages, n):
+    """More rows and a larger max_chunk than the sequences have (one captured call for every batch), and few
+    sequences with long contexts (keys cut, parts joined)."""
+    c = Case(L8, pages, [n, 1, 0], [3000, 2, 0], seed=4, tail=60)
+    c.batch = ChunkBatch(_dev(c.starts), _dev(c.ctx), _dev(c.table), c.rows, c.rows)
+    c.ws = chunk_workspace(c.desc, c.batch)
+    vals = c.fill_context()
+    q = torch.as_tensor(c.rng.normal(size=(c.rows, 32, 128))).to("cuda", torch.bfloat16)
+    out = torch.full((c.rows, 4096), -7.0, dtype=torch.bfloat16, device="cuda")
+    chunk_attn(c.desc, c.layer, c.batch, q, out, c.ws)
+    assert c.error() == 0 and (out[c.starts[-1]:] == -7).all()
+    _check_attn(c, q, out, vals)
