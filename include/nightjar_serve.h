@@ -66,8 +66,8 @@ typedef struct nj_kv_layer {
  *
  *   starts        device int32 [B+1], not decreasing, 0 <= starts[0], starts[B] <= rows
  *   context_lens  device int32 [B], not modified
- *   block_table   device int32 [B][max_blocks]
- *   rows          rows of the row arrays (>= 1)
+ *   block_table   device int32 [B][max_blocks], max_blocks <= 2^21
+ *   B, rows       1 <= B <= 2^20, 1 <= rows <= 2^24: rows of the row arrays
  *   max_chunk     no sequence has more new tokens than this (1 <= max_chunk <= rows)
  *
  * A sequence that breaks these rules, or whose positions do not fit the block

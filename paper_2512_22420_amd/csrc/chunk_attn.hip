@@ -25,9 +25,13 @@ struct ChunkAttnK {
   void* out;
   int H, Hkv, D;
   float scale_log2;
+  int G, tokens;      // query heads per KV head, tokens of a tile (kTileRows / G)
+  int cap[2];         // pieces per KV head up to which keys are cut, by class
+  int min_cut[2];     // shortest run of keys
   int threshold;      // sequences of more than this many query rows per KV head are cut into tiles, others streamed
   float* part_o[2];   // per class: [slot][rows of the class][kHD], unnormalised
-  float2* part_ml[2]; // [slot][rows]: max (log2 domain), sum
+  float* part_ml[2];  // [slot][rows][2]: max (log2 domain), sum
+  int* counters[2];   // [slot][kCounterStride]: parts done, at a tile's first slot; zero between calls
 };
 
 // ---------------------------------------------------------------------------
@@ -35,121 +39,118 @@ struct ChunkAttnK {
 // heads that share it, tokens first.  Class kTiles cuts them into tiles of up to
 // 128 rows (whole tokens), class kStream takes sequences of up to 32 rows whole.
 // When a class has fewer pieces than the chip takes, the keys of each piece are
-// cut too, and a merge joins the parts: the cut length L is the same for all
-// sequences of the class, the smallest of maxlen / 1, 2, 3, 4, 6, .. whose pieces
-// still fit kSlots.  Every workgroup works this out by itself from starts and
-// context lengths (a few loads per 64 sequences) instead of reading a list that
-// another kernel would have to write first.
+// cut too, into runs of at most L tokens, L the same for the whole class: with T
+// tiles that see W keys in all, runs of W / cap fit cap pieces if their ends
+// round well, and runs of W / (cap - T) always do.  The last part of a tile to be
+// done joins them.  Every workgroup works this out by itself from starts and
+// context lengths (one round of loads per 64 sequences, sums by DPP) instead of
+// reading a list that another kernel would have to write first.
 // ---------------------------------------------------------------------------
 enum { kTiles = 0, kStream = 1 };
 constexpr int kTileRows = 128, kStreamRows = 32;
-constexpr int kSlots[2] = {512, 1024};      // pieces (over all KV heads) up to which keys are cut
-constexpr int kMinCut[2] = {256, 128};      // tokens
-constexpr int kCuts = 12;
-__device__ constexpr int kCutBy[kCuts] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+constexpr int kSlots[2] = {512, 1024};  // pieces (over all KV heads) up to which keys are cut
+constexpr int kMinCut[2] = {256, 128};  // tokens
 
 struct Piece {
   ChunkSeq s;
-  int tile;          // first token tile * tokens
+  int tile;  // first token tile * tokens
   int split, nsplit;
-  int slot;          // of split 0 (nsplit > 1)
+  int slot;  // of split 0 (nsplit > 1)
   int b;
 };
 
-__device__ __forceinline__ int wave_sum_i(int v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+// Sum over the lanes up to this one: within rows of 16 lanes, then across them.
+__device__ __forceinline__ int wave_scan_i(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // row_shr:1
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);  // row_shr:2
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);  // row_shr:4
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);  // row_shr:8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row_bcast:15
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // row_bcast:31
   return v;
 }
-__device__ __forceinline__ int wave_max_i(int v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = max(v, __shfl_xor(v, o));
-  return v;
-}
-__device__ __forceinline__ int wave_scan_i(int v) {  // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const int up = __shfl_up(v, o);
-    if (lane >= o) v += up;
-  }
-  return v;
+__device__ __forceinline__ int wave_sum_i(int v) { return __builtin_amdgcn_readlane(wave_scan_i(v), 63); }
+__device__ __forceinline__ int wave_max_i(int v) {  // v >= 0
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));
+  return __builtin_amdgcn_readlane(v, 63);
 }
 
 // Tiles of a sequence in class C (0: not of this class).
 template <int C>
-__device__ __forceinline__ int class_tiles(const ChunkAttnK& a, const ChunkSeq& s, int G, int tokens) {
-  if (s.n == 0 || (s.n * G > a.threshold) != (C == kTiles)) return 0;
-  return C == kTiles ? (s.n + tokens - 1) / tokens : 1;
+__device__ __forceinline__ int class_tiles(const ChunkAttnK& a, const ChunkSeq& s) {
+  if (s.n == 0 || (s.n * a.G > a.threshold) != (C == kTiles)) return 0;
+  return C == kTiles ? (s.n + a.tokens - 1) / a.tokens : 1;
 }
 
-// Piece `item` of class C (per KV head), or with by_tile the split tile number
-// `item`, with slot and nsplit of all its pieces.  Run by whole waves, the same
-// in each; false if there is none.
+// Piece `item` of class C (per KV head).  Run by whole waves, the same in each;
+// false if there is none.
 template <int C>
-__device__ bool find_piece(const ChunkAttnK& a, int item, bool by_tile, Piece& out) {
-  const int lane = threadIdx.x & 63, G = a.H / a.Hkv, B = a.c.B, tokens = kTileRows / G;
-  const int cap = kSlots[C] / a.Hkv;
-  // total tiles and the longest key range of the class
-  int tiles = 0, longest = 0;
+__device__ bool find_piece(const ChunkAttnK& a, int item, Piece& out) {
+  const int lane = threadIdx.x & 63, B = a.c.B, cap = a.cap[C];
+  // the class's tiles, the keys that they see (in units of 16, at most), and the longest range
+  int tiles = 0, keys = 0, longest = 0, t0 = 0;
   ChunkSeq s0{0, 0, 0, false};
-  int t0 = 0;
   for (int b0 = 0; b0 < B; b0 += kWave) {
     const int b = b0 + lane;
     const ChunkSeq s = b < B ? chunk_seq(a.c, b) : ChunkSeq{0, 0, 0, false};
-    const int t = class_tiles<C>(a, s, G, tokens);
+    const int t = class_tiles<C>(a, s);
     if (b0 == 0) {
       s0 = s;
       t0 = t;
     }
     tiles += t;
+    keys += t * ((s.c + s.n + 15) >> 4);
     longest = max(longest, t ? s.c + s.n : 0);
   }
   tiles = wave_sum_i(tiles);
-  longest = wave_max_i(longest);
   if (tiles == 0) return false;
-  // the cut
+  longest = wave_max_i(longest);
+  auto seq = [&](int b0, int& t) {
+    const int b = b0 + lane;
+    const ChunkSeq s = b0 == 0 ? s0 : b < B ? chunk_seq(a.c, b) : ChunkSeq{0, 0, 0, false};
+    t = b0 == 0 ? t0 : class_tiles<C>(a, s);
+    return s;
+  };
   int L = longest;
-  if (tiles * 2 <= cap) {
-    int cnt[kCuts] = {};
+  if (tiles * 2 <= cap && longest > kMinCut[C]) {
+    // (at most 2^9 tiles of 2^21 blocks: no sum leaves 32 bits)
+    keys = wave_sum_i(keys);
+    const auto cut = [&](int pieces) { return max((int)((int64_t)keys * 16 / pieces) + 1, a.min_cut[C]); };
+    L = cut(cap);
+    int cnt = 0;
     for (int b0 = 0; b0 < B; b0 += kWave) {
-      const int b = b0 + lane;
-      const ChunkSeq s = b0 == 0 ? s0 : b < B ? chunk_seq(a.c, b) : ChunkSeq{0, 0, 0, false};
-      const int t = b0 == 0 ? t0 : class_tiles<C>(a, s, G, tokens);
-      if (t) {
-#pragma unroll
-        for (int k = 1; k < kCuts; ++k) {
-          const int l = max((longest + kCutBy[k] - 1) / kCutBy[k], kMinCut[C]);
-          cnt[k] += t * ((s.c + s.n + l - 1) / l);
-        }
-      }
+      int t;
+      const ChunkSeq s = seq(b0, t);
+      cnt += t ? t * ((s.c + s.n + L - 1) / L) : 0;
     }
-#pragma unroll
-    for (int k = 1; k < kCuts; ++k)
-      if (wave_sum_i(cnt[k]) <= cap) L = max((longest + kCutBy[k] - 1) / kCutBy[k], kMinCut[C]);
+    if (wave_sum_i(cnt) > cap) L = cut(cap - tiles);
   }
   // the piece
   int before = 0, slots = 0;
   for (int b0 = 0; b0 < B; b0 += kWave) {
-    const int b = b0 + lane;
-    const ChunkSeq s = b0 == 0 ? s0 : b < B ? chunk_seq(a.c, b) : ChunkSeq{0, 0, 0, false};
-    const int t = b0 == 0 ? t0 : class_tiles<C>(a, s, G, tokens);
+    int t;
+    const ChunkSeq s = seq(b0, t);
     const int ns = t ? (s.c + s.n + L - 1) / L : 0;
-    const int sl = ns > 1 ? t * ns : 0, mine = by_tile ? (ns > 1 ? t : 0) : t * ns;
+    const int mine = t * ns, sl = ns > 1 ? mine : 0;
     const int inc = wave_scan_i(mine), sinc = wave_scan_i(sl);
     const uint64_t hit = __ballot(before + inc > item);
     if (hit) {
       // (the same in every lane: kept in scalar registers)
       const int l = __builtin_amdgcn_readfirstlane(__ffsll((long long)hit) - 1);
       auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
-      const int at = item - (before + of(inc - mine)), nt = of(t);
+      const int at = item - (before + of(inc - mine));
       out.b = b0 + l;
       out.s = {of(s.s0), of(s.n), of(s.c), false};
       out.nsplit = of(ns);
       // the last tiles see the most keys: they go first
-      const int rank = by_tile ? at : at / out.nsplit;
-      out.tile = __builtin_amdgcn_readfirstlane(nt - 1 - rank);
-      out.split = __builtin_amdgcn_readfirstlane(by_tile ? 0 : at % out.nsplit);
+      const int rank = at / out.nsplit;
+      out.tile = __builtin_amdgcn_readfirstlane(of(t) - 1 - rank);
+      out.split = __builtin_amdgcn_readfirstlane(at % out.nsplit);
       out.slot = __builtin_amdgcn_readfirstlane(slots + of(sinc - sl) + rank * out.nsplit);
       return true;
     }
@@ -329,13 +330,102 @@ __global__ __launch_bounds__(256) void chunk_attn_row_kernel(ChunkAttnK a) {
   }
 }
 
+// Parts of a tile whose keys were cut: written and read past the caches of the XCDs
+// (device-coherent accesses, as between the parts of a split GEMM tile), counted in
+// at the tile's first slot, and joined by the last to arrive:
+//   out = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s.
+template <int C>
+struct Parts {
+  static constexpr int ROWS = C == kTiles ? kTileRows : kStreamRows;
+  __amdgpu_buffer_rsrc_t o, ml;
+  __device__ __forceinline__ Parts(const ChunkAttnK& a)
+      : o(coherent_rsrc(a.part_o[C], kSlots[C] * ROWS * kHD * 4)), ml(coherent_rsrc(a.part_ml[C], kSlots[C] * ROWS * 8)) {}
+  __device__ __forceinline__ uint32_t row(const ChunkAttnK& a, const Piece& pc, int split, int kvh, int r) const {
+    return (uint32_t)(((pc.slot + split) * a.Hkv + kvh) * ROWS + r);
+  }
+  __device__ __forceinline__ void put(uint32_t row, int d, f32x4 v) const { coherent_store(o, (row * kHD + d) * 4, v); }
+  __device__ __forceinline__ void put_ml(uint32_t row, float m, float l) const {
+    coherent_store_f32(ml, row * 8, m);
+    coherent_store_f32(ml, row * 8 + 4, l);
+  }
+};
+
+constexpr int kJoinSplits = 4, kJoinUnits = 4;  // loads in flight per thread: parts of one unit (4 dims of a row), units
+template <int C>
+__device__ void join_parts(const ChunkAttnK& a, const Piece& pc, int kvh, int tokens, const Parts<C>& parts) {
+  __shared__ int s_last;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this thread's part is written
+  __syncthreads();
+  int* cnt = a.counters[C] + (size_t)(pc.slot * a.Hkv + kvh) * kCounterStride;
+  if (threadIdx.x == 0)
+    s_last = __hip_atomic_fetch_add(cnt, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == pc.nsplit - 1;
+  __syncthreads();
+  if (!s_last) return;
+  if (threadIdx.x == 0) __hip_atomic_store(cnt, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  const int i0 = pc.tile * tokens, R = min(tokens, pc.s.n - i0) * a.G, units = R * (kHD / 4);
+  for (int u0 = 0; u0 < units; u0 += 256 * kJoinUnits) {
+    f32x4 acc[kJoinUnits];
+    float mx[kJoinUnits], sum[kJoinUnits];
+#pragma unroll
+    for (int q = 0; q < kJoinUnits; ++q) {
+      acc[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+      mx[q] = -INFINITY;
+      sum[q] = 0.f;
+    }
+    for (int s0 = 0; s0 < pc.nsplit; s0 += kJoinSplits) {
+      f32x4 ov[kJoinUnits][kJoinSplits];
+      float2 ml[kJoinUnits][kJoinSplits];
+#pragma unroll
+      for (int q = 0; q < kJoinUnits; ++q) {
+        if (u0 + q * 256 >= units) break;  // uniform
+        const int u = min(u0 + q * 256 + (int)threadIdx.x, units - 1);
+#pragma unroll
+        for (int j = 0; j < kJoinSplits; ++j) {
+          const uint32_t row = parts.row(a, pc, min(s0 + j, pc.nsplit - 1), kvh, u / (kHD / 4));
+          ml[q][j] = coherent_load_f32x2(parts.ml, row * 8);
+          ov[q][j] = coherent_load(parts.o, (row * kHD + (u % (kHD / 4)) * 4) * 4);
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < kJoinUnits; ++q) {
+        if (u0 + q * 256 >= units) break;
+        float mn = mx[q];
+#pragma unroll
+        for (int j = 0; j < kJoinSplits; ++j)
+          if (s0 + j < pc.nsplit) mn = fmaxf(mn, ml[q][j].x);
+        // (a part without keys, or with nothing but NaN scores, has m = -inf: weight 0, and its NaN stays)
+        const float f = mx[q] == -INFINITY ? 0.f : exp2f(mx[q] - mn);
+        acc[q] *= f;
+        sum[q] *= f;
+        mx[q] = mn;
+#pragma unroll
+        for (int j = 0; j < kJoinSplits; ++j)
+          if (s0 + j < pc.nsplit) {
+            const float w = ml[q][j].x == -INFINITY ? 0.f : exp2f(ml[q][j].x - mn);
+            sum[q] += w * ml[q][j].y;
+            acc[q] += w * ov[q][j];
+          }
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < kJoinUnits; ++q) {
+      const int u = u0 + q * 256 + (int)threadIdx.x;
+      if (u >= units) break;
+      const int r = u / (kHD / 4), d = (u % (kHD / 4)) * 4;
+      const float inv = 1.0f / sum[q];
+      bf16_t* dst = static_cast<bf16_t*>(a.out) + ((size_t)(pc.s.s0 + i0 + r / a.G) * a.H + kvh * a.G + r % a.G) * kHD + d;
+      *reinterpret_cast<u32x2*>(dst) = u32x2{pack_bf16x2(acc[q][0] * inv, acc[q][1] * inv), pack_bf16x2(acc[q][2] * inv, acc[q][3] * inv)};
+    }
+  }
+}
+
 // A piece whose masked tokens hold NaN or infinities in V (a later token of the
 // chunk, seen by some of its rows): in the matrix products 0 times those would
 // reach the rows that do not see them.  The piece's rows again, one at a time, each
 // over the keys that it sees.
 template <int PT, int C>
-__device__ void redo_piece(const ChunkAttnK& a, const Piece& pc, int kvh, int G, int tokens, int k0, int k1, char* lds) {
-  constexpr int ROWS = C == kTiles ? kTileRows : kStreamRows;
+__device__ void redo_piece(const ChunkAttnK& a, const Piece& pc, int kvh, int G, int tokens, int k0, int k1, char* lds,
+                           const Parts<C>& parts) {
   RowLds& sh = *reinterpret_cast<RowLds*>(lds);
   const int i0 = pc.tile * tokens, R = min(tokens, pc.s.n - i0) * G;
   for (int r = 0; r < R; ++r) {
@@ -347,9 +437,9 @@ __device__ void redo_piece(const ChunkAttnK& a, const Piece& pc, int kvh, int G,
     if (pc.nsplit == 1) {
       static_cast<bf16_t*>(a.out)[at + threadIdx.x] = f2bf(o[0] / l);
     } else {
-      const size_t slot = ((size_t)(pc.slot + pc.split) * a.Hkv + kvh) * ROWS + r;
-      a.part_o[C][slot * kHD + threadIdx.x] = o[0];
-      if (threadIdx.x == 0) a.part_ml[C][slot] = float2{m, l};
+      const uint32_t prow = parts.row(a, pc, pc.split, kvh, r);
+      coherent_store_f32(parts.o, (prow * kHD + threadIdx.x) * 4, o[0]);
+      if (threadIdx.x == 0) parts.put_ml(prow, m, l);
     }
   }
 }
@@ -390,8 +480,8 @@ __global__ __launch_bounds__(256, 2) void chunk_tile_kernel(ChunkAttnK a) {
   const int kvh = __builtin_amdgcn_readfirstlane(blockIdx.x % a.Hkv);
   if (blockIdx.x == 0) chunk_check(a.c);
   Piece pc;
-  if (!find_piece<kTiles>(a, blockIdx.x / a.Hkv, false, pc)) return;
-  const int G = __builtin_amdgcn_readfirstlane(a.H / a.Hkv), tokens = __builtin_amdgcn_readfirstlane(kTileRows / G);
+  if (!find_piece<kTiles>(a, blockIdx.x / a.Hkv, pc)) return;
+  const int G = a.G, tokens = a.tokens;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r32 = lane & 31, h = lane >> 5;
   const int i0 = pc.tile * tokens, len = pc.s.c + min(i0 + tokens, pc.s.n);
@@ -568,24 +658,22 @@ __global__ __launch_bounds__(256, 2) void chunk_tile_kernel(ChunkAttnK a) {
     if (it + 1 < nit) convert(it + 1);
   }
   if (__builtin_amdgcn_ballot_w64(bad) && lane == 0) flag_error(a.c.err, kErrBlock);
-  if (__syncthreads_or(odd)) {
-    redo_piece<PT, kTiles>(a, pc, kvh, G, tokens, k0, k1, smem);
-    return;
-  }
+  const Parts<kTiles> parts(a);
   const float l = l_run + __shfl_xor(l_run, 32);
-  if (pc.nsplit == 1) {
+  if (__syncthreads_or(odd)) {
+    redo_piece<PT, kTiles>(a, pc, kvh, G, tokens, k0, k1, smem, parts);
+  } else if (pc.nsplit == 1) {
     if (row_ok) store_row(a, row, head, o, 1.0f / l);
-    return;
+  } else if (row_ok) {
+    const uint32_t prow = parts.row(a, pc, pc.split, kvh, r);
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        parts.put(prow, 32 * dt + 8 * j + 4 * h, f32x4{o[dt][4 * j], o[dt][4 * j + 1], o[dt][4 * j + 2], o[dt][4 * j + 3]});
+    if (h == 0) parts.put_ml(prow, m_run, l);
   }
-  if (!row_ok) return;
-  const size_t slot = ((size_t)(pc.slot + pc.split) * a.Hkv + kvh) * kTileRows + r;
-  float* dst = a.part_o[kTiles] + slot * kHD + 4 * h;
-#pragma unroll
-  for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      *reinterpret_cast<f32x4*>(dst + 32 * dt + 8 * j) = f32x4{o[dt][4 * j], o[dt][4 * j + 1], o[dt][4 * j + 2], o[dt][4 * j + 3]};
-  if (h == 0) a.part_ml[kTiles][slot] = float2{m_run, l};
+  if (pc.nsplit > 1) join_parts<kTiles>(a, pc, kvh, tokens, parts);
 }
 
 // ---------------------------------------------------------------------------
@@ -631,8 +719,8 @@ __global__ __launch_bounds__(256, 2) void chunk_stream_kernel(ChunkAttnK a) {
   const int kvh = __builtin_amdgcn_readfirstlane(blockIdx.x % a.Hkv);
   if (blockIdx.x == 0) chunk_check(a.c);
   Piece pc;
-  if (!find_piece<kStream>(a, blockIdx.x / a.Hkv, false, pc)) return;
-  const int G = __builtin_amdgcn_readfirstlane(a.H / a.Hkv), R = pc.s.n * G, len = pc.s.c + pc.s.n;
+  if (!find_piece<kStream>(a, blockIdx.x / a.Hkv, pc)) return;
+  const int G = a.G, R = pc.s.n * G, len = pc.s.c + pc.s.n;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r16 = lane & 15, g = lane >> 4;
   int k0, k1;
@@ -841,8 +929,10 @@ __global__ __launch_bounds__(256, 2) void chunk_stream_kernel(ChunkAttnK a) {
   }
   if (__builtin_amdgcn_ballot_w64(bad) && lane == 0) flag_error(a.c.err, kErrBlock);
 
+  const Parts<kStream> parts(a);
   if (__syncthreads_or(odd)) {
-    redo_piece<PT, kStream>(a, pc, kvh, G, pc.s.n, k0, k1, reinterpret_cast<char*>(s_o));
+    redo_piece<PT, kStream>(a, pc, kvh, G, pc.s.n, k0, k1, reinterpret_cast<char*>(s_o), parts);
+    if (pc.nsplit > 1) join_parts<kStream>(a, pc, kvh, pc.s.n, parts);
     return;
   }
   // join the waves, then store the rows or this split's part
@@ -878,39 +968,12 @@ __global__ __launch_bounds__(256, 2) void chunk_stream_kernel(ChunkAttnK a) {
       bf16_t* dst = static_cast<bf16_t*>(a.out) + ((size_t)(pc.s.s0 + rr / G) * a.H + kvh * G + rr % G) * kHD + d;
       *reinterpret_cast<u32x2*>(dst) = u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
     } else {
-      const size_t slot = ((size_t)(pc.slot + pc.split) * a.Hkv + kvh) * kStreamRows + rr;
-      *reinterpret_cast<f32x4*>(a.part_o[kStream] + slot * kHD + d) = acc;
-      if (d == 0) a.part_ml[kStream][slot] = float2{mx, sum};
+      const uint32_t prow = parts.row(a, pc, pc.split, kvh, rr);
+      parts.put(prow, d, acc);
+      if (d == 0) parts.put_ml(prow, mx, sum);
     }
   }
-}
-
-// Joins the parts of pieces whose keys were cut:
-//   out = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s.
-// grid (split tiles of the class per KV head * Hkv, row groups of 8); 4 dims of a row per thread.
-template <int C>
-__global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkAttnK a) {
-  constexpr int ROWS = C == kTiles ? kTileRows : kStreamRows;
-  const int kvh = __builtin_amdgcn_readfirstlane(blockIdx.x % a.Hkv);
-  Piece pc;
-  if (!find_piece<C>(a, blockIdx.x / a.Hkv, true, pc)) return;
-  const int G = a.H / a.Hkv, tokens = C == kTiles ? kTileRows / G : pc.s.n;
-  const int r = blockIdx.y * 8 + threadIdx.x / (kHD / 4), d = (threadIdx.x % (kHD / 4)) * 4, i = pc.tile * tokens + r / G;
-  if (r >= tokens * G || i >= pc.s.n) return;
-  const size_t base = ((size_t)pc.slot * a.Hkv + kvh) * ROWS + r, step = (size_t)a.Hkv * ROWS;
-  float mx = -INFINITY;
-  for (int s = 0; s < pc.nsplit; ++s) mx = fmaxf(mx, a.part_ml[C][base + s * step].x);
-  f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
-  float sum = 0.f;
-  for (int s = 0; s < pc.nsplit; ++s) {
-    const float2 ml = a.part_ml[C][base + s * step];
-    const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - mx);
-    sum += f * ml.y;
-    acc += f * *reinterpret_cast<const f32x4*>(a.part_o[C] + (base + s * step) * kHD + d);
-  }
-  const float inv = 1.0f / sum;
-  bf16_t* dst = static_cast<bf16_t*>(a.out) + ((size_t)(pc.s.s0 + i) * a.H + kvh * G + r % G) * kHD + d;
-  *reinterpret_cast<u32x2*>(dst) = u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
+  if (pc.nsplit > 1) join_parts<kStream>(a, pc, kvh, pc.s.n, parts);
 }
 
 }  // namespace
@@ -949,7 +1012,7 @@ bool chunk_args(const char* what, const nj_model_desc* d, const nj_kv_layer* kv,
   if (!batch_sizes(what, bt->B, bt->rows, bt->max_chunk)) return false;
   if (bt->max_blocks < 1 || kv->num_blocks < 1)
     return !set_last_error(NJ_EINVAL, "%s: max_blocks and num_blocks must be >= 1", what);
-  if (bt->max_blocks > (1 << 26)) return !set_last_error(NJ_EINVAL, "%s: max_blocks > 2^26", what);
+  if (bt->max_blocks > (1 << 21)) return !set_last_error(NJ_EINVAL, "%s: max_blocks > 2^21", what);
   if (!bt->starts || !bt->context_lens || !bt->block_table || !kv->k || !kv->v)
     return !set_last_error(NJ_EINVAL, "%s: a required pointer is NULL", what);
   const bool pages_ok = d->dtype == NJ_F32 ? kv->dtype == NJ_F32 : kv->dtype == NJ_BF16 || kv->dtype == NJ_E4M3;
@@ -974,7 +1037,7 @@ constexpr size_t kErrBytes = 256;
 // Workspace of the attention: [error word][parts of the tiles][parts of the streamed pieces].
 struct AttnParts {
   bool tiles, stream;
-  size_t o[2], ml[2], total;
+  size_t o[2], ml[2], cnt[2], total;
 };
 AttnParts attn_parts(const nj_model_desc& d, int max_chunk) {
   AttnParts p{};
@@ -989,7 +1052,8 @@ AttnParts attn_parts(const nj_model_desc& d, int max_chunk) {
     if (used[c]) {
       p.o[c] = p.total;
       p.ml[c] = p.o[c] + (size_t)kSlots[c] * rows[c] * kHD * 4;
-      p.total = p.ml[c] + (size_t)kSlots[c] * rows[c] * 8;
+      p.cnt[c] = p.ml[c] + (size_t)kSlots[c] * rows[c] * 8;
+      p.total = p.cnt[c] + (size_t)kSlots[c] * kCounterStride * 4;
     }
   return p;
 }
@@ -1000,7 +1064,7 @@ AttnParts attn_parts(const nj_model_desc& d, int max_chunk) {
 // the batch can hold no short sequence (or only by padding), the tiles take
 // everything, and one launch is saved.
 hipError_t launch_chunk_attn(ChunkAttnK& a, const AttnParts& p, int pt, int B, int rows, int max_chunk, hipStream_t s) {
-  const int G = a.H / a.Hkv;
+  const int G = a.G;
   if (pt == kPageF32 || G > kTileRows) {
     auto kern = pt == kPageF32    ? chunk_attn_row_kernel<kPageF32, float>
                 : pt == kPageBF16 ? chunk_attn_row_kernel<kPageBF16, bf16_t>
@@ -1013,26 +1077,17 @@ hipError_t launch_chunk_attn(ChunkAttnK& a, const AttnParts& p, int pt, int B, i
   a.threshold = all_long ? 0 : p.tiles ? 16 : INT_MAX;
   hipError_t e = hipSuccess;
   if (p.tiles) {
-    const int tokens = kTileRows / G, pieces = std::max(rows / tokens + std::min(B, rows), kSlots[kTiles] / a.Hkv);
+    const int pieces = std::max(rows / a.tokens + std::min(B, rows), a.cap[kTiles]);
     hipLaunchKernelGGL(pt == kPageE4M3 ? chunk_tile_kernel<kPageE4M3> : chunk_tile_kernel<kPageBF16>, dim3(pieces * a.Hkv),
                        dim3(256), 0, s, a);
     e = hipGetLastError();
-    if (e == hipSuccess && kSlots[kTiles] / a.Hkv >= 2) {
-      hipLaunchKernelGGL(chunk_merge_kernel<kTiles>, dim3(kSlots[kTiles] / a.Hkv / 2 * a.Hkv, kTileRows / 8), dim3(256), 0, s, a);
-      e = hipGetLastError();
-    }
   }
   if (!all_long && e == hipSuccess) {
-    const int pieces = std::max(std::min(B, rows), kSlots[kStream] / a.Hkv);
+    const int pieces = std::max(std::min(B, rows), a.cap[kStream]);
     auto kern = pt == kPageE4M3 ? (one_tile ? chunk_stream_kernel<kPageE4M3, 1> : chunk_stream_kernel<kPageE4M3, 2>)
                                 : (one_tile ? chunk_stream_kernel<kPageBF16, 1> : chunk_stream_kernel<kPageBF16, 2>);
     hipLaunchKernelGGL(kern, dim3(pieces * a.Hkv), dim3(256), 0, s, a);
     e = hipGetLastError();
-    const int split = std::min(std::min(B, rows), kSlots[kStream] / a.Hkv / 2);
-    if (e == hipSuccess && split > 0) {
-      hipLaunchKernelGGL(chunk_merge_kernel<kStream>, dim3(split * a.Hkv, kStreamRows / 8), dim3(256), 0, s, a);
-      e = hipGetLastError();
-    }
   }
   return e;
 }
@@ -1102,10 +1157,15 @@ int nightjar_chunk_attn(const nj_model_desc* desc, const nj_kv_layer* kv, const 
   a.H = d.n_heads;
   a.Hkv = d.n_kv_heads;
   a.D = d.head_dim;
+  a.G = d.n_heads / d.n_kv_heads;
+  a.tokens = kTileRows / a.G;
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)d.head_dim);
   for (int k = 0; k < 2; ++k) {
     a.part_o[k] = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.o[k]);
-    a.part_ml[k] = reinterpret_cast<float2*>(static_cast<char*>(workspace) + p.ml[k]);
+    a.part_ml[k] = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.ml[k]);
+    a.counters[k] = reinterpret_cast<int*>(static_cast<char*>(workspace) + p.cnt[k]);
+    a.cap[k] = kSlots[k] / d.n_kv_heads;
+    a.min_cut[k] = kMinCut[k];
   }
   const hipError_t e = launch_chunk_attn(a, p, page_type(kv), batch->B, batch->rows, batch->max_chunk, (hipStream_t)stream);
   return e == hipSuccess ? NJ_OK : set_last_error(NJ_EHIP, "chunk_attn: %s", hipGetErrorString(e));
