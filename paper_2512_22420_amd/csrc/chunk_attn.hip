@@ -26,6 +26,7 @@ struct ChunkAttnK {
   int H, Hkv, D;
   float scale_log2;
   int G, tokens;      // query heads per KV head, tokens of a tile (kTileRows / G)
+  float inv_tokens;   // 1 / tokens
   int cap[2];         // pieces per KV head up to which keys are cut, by class
   int min_cut[2];     // shortest run of keys
   int threshold;      // sequences of more than this many query rows per KV head are cut into tiles, others streamed
@@ -80,15 +81,21 @@ __device__ __forceinline__ int wave_max_i(int v) {  // v >= 0
   return __builtin_amdgcn_readlane(v, 63);
 }
 
+// ceil(x / L) for 0 <= x < 2^26 and L >= 1 with inv = 1 / L in fp32: the quotient is
+// off by one at most, which the products tell.
+__device__ __forceinline__ int ceil_div(int x, int L, float inv) {
+  const int q = (int)((float)x * inv), d = x - q * L;
+  return q + (d > 0 ? 1 : 0) + (d > L ? 1 : 0) - (d <= -L ? 1 : 0);
+}
+
 // Tiles of a sequence in class C (0: not of this class).
 template <int C>
 __device__ __forceinline__ int class_tiles(const ChunkAttnK& a, const ChunkSeq& s) {
   if (s.n == 0 || (s.n * a.G > a.threshold) != (C == kTiles)) return 0;
-  return C == kTiles ? (s.n + a.tokens - 1) / a.tokens : 1;
+  return C == kTiles ? ceil_div(s.n, a.tokens, a.inv_tokens) : 1;
 }
 
-// Piece `item` of class C (per KV head).  Run by whole waves, the same in each;
-// false if there is none.
+// Piece `item` of class C (per KV head); false if there is none.  Run by one wave.
 template <int C>
 __device__ bool find_piece(const ChunkAttnK& a, int item, Piece& out) {
   const int lane = threadIdx.x & 63, B = a.c.B, cap = a.cap[C];
@@ -123,19 +130,21 @@ __device__ bool find_piece(const ChunkAttnK& a, int item, Piece& out) {
     const auto cut = [&](int pieces) { return max((int)((int64_t)keys * 16 / pieces) + 1, a.min_cut[C]); };
     L = cut(cap);
     int cnt = 0;
+    const float inv = 1.0f / (float)L;
     for (int b0 = 0; b0 < B; b0 += kWave) {
       int t;
       const ChunkSeq s = seq(b0, t);
-      cnt += t ? t * ((s.c + s.n + L - 1) / L) : 0;
+      cnt += t ? t * ceil_div(s.c + s.n, L, inv) : 0;
     }
     if (wave_sum_i(cnt) > cap) L = cut(cap - tiles);
   }
   // the piece
   int before = 0, slots = 0;
+  const float inv = 1.0f / (float)L;
   for (int b0 = 0; b0 < B; b0 += kWave) {
     int t;
     const ChunkSeq s = seq(b0, t);
-    const int ns = t ? (s.c + s.n + L - 1) / L : 0;
+    const int ns = t ? ceil_div(s.c + s.n, L, inv) : 0;
     const int mine = t * ns, sl = ns > 1 ? mine : 0;
     const int inc = wave_scan_i(mine), sinc = wave_scan_i(sl);
     const uint64_t hit = __ballot(before + inc > item);
@@ -158,6 +167,25 @@ __device__ bool find_piece(const ChunkAttnK& a, int item, Piece& out) {
     slots += __builtin_amdgcn_readlane(sinc, 63);
   }
   return false;
+}
+
+// The workgroup's piece: found by its first wave.
+template <int C>
+__device__ __forceinline__ bool wg_piece(const ChunkAttnK& a, int item, Piece& pc) {
+  __shared__ int s_pc[9];
+  if (threadIdx.x < kWave) {
+    Piece p{};
+    const bool ok = find_piece<C>(a, item, p);
+    if (threadIdx.x == 0) {
+      const int v[9] = {p.s.s0, p.s.n, p.s.c, p.tile, p.split, p.nsplit, p.slot, p.b, ok};
+#pragma unroll
+      for (int i = 0; i < 9; ++i) s_pc[i] = v[i];
+    }
+  }
+  __syncthreads();
+  auto of = [&](int i) { return __builtin_amdgcn_readfirstlane(s_pc[i]); };
+  pc = {{of(0), of(1), of(2), false}, of(3), of(4), of(5), of(6), of(7)};
+  return of(8) != 0;
 }
 
 // Keys of split `split` of a piece that sees `len` keys: whole steps of 64.
@@ -350,9 +378,14 @@ struct Parts {
   }
 };
 
-constexpr int kJoinSplits = 4, kJoinUnits = 4;  // loads in flight per thread: parts of one unit (4 dims of a row), units
+// A thread joins units of 4 dims of a row.  Tiles have many units and few parts:
+// four units at once, four parts of each in flight.  Streamed pieces have few units
+// and up to a hundred parts: one unit, 16 parts in flight, and where the rows leave
+// threads over, these take parts of their own (part p to group p % groups) and meet
+// in LDS (8 KB).
 template <int C>
-__device__ void join_parts(const ChunkAttnK& a, const Piece& pc, int kvh, int tokens, const Parts<C>& parts) {
+__device__ void join_parts(const ChunkAttnK& a, const Piece& pc, int kvh, int tokens, const Parts<C>& parts, char* lds) {
+  constexpr int NU = C == kTiles ? 4 : 1, NJ = C == kTiles ? 4 : 16;
   __shared__ int s_last;
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this thread's part is written
   __syncthreads();
@@ -363,58 +396,81 @@ __device__ void join_parts(const ChunkAttnK& a, const Piece& pc, int kvh, int to
   if (!s_last) return;
   if (threadIdx.x == 0) __hip_atomic_store(cnt, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   const int i0 = pc.tile * tokens, R = min(tokens, pc.s.n - i0) * a.G, units = R * (kHD / 4);
-  for (int u0 = 0; u0 < units; u0 += 256 * kJoinUnits) {
-    f32x4 acc[kJoinUnits];
-    float mx[kJoinUnits], sum[kJoinUnits];
+  const int groups = C == kTiles ? 1 : max(1, 256 / units);
+  const int grp = groups > 1 ? (int)threadIdx.x / units : 0, t0 = groups > 1 ? (int)threadIdx.x % units : (int)threadIdx.x;
+  auto write = [&](int u, f32x4 acc, float sum) {
+    const int r = u / (kHD / 4), d = (u % (kHD / 4)) * 4;
+    const float inv = 1.0f / sum;
+    bf16_t* dst = static_cast<bf16_t*>(a.out) + ((size_t)(pc.s.s0 + i0 + r / a.G) * a.H + kvh * a.G + r % a.G) * kHD + d;
+    *reinterpret_cast<u32x2*>(dst) = u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
+  };
+  for (int u0 = 0; u0 < units; u0 += 256 * NU) {
+    f32x4 acc[NU];
+    float mx[NU], sum[NU];
 #pragma unroll
-    for (int q = 0; q < kJoinUnits; ++q) {
+    for (int q = 0; q < NU; ++q) {
       acc[q] = f32x4{0.f, 0.f, 0.f, 0.f};
       mx[q] = -INFINITY;
       sum[q] = 0.f;
     }
-    for (int s0 = 0; s0 < pc.nsplit; s0 += kJoinSplits) {
-      f32x4 ov[kJoinUnits][kJoinSplits];
-      float2 ml[kJoinUnits][kJoinSplits];
+    for (int s0 = grp; s0 < pc.nsplit; s0 += groups * NJ) {
+      f32x4 ov[NU][NJ];
+      float2 ml[NU][NJ];
 #pragma unroll
-      for (int q = 0; q < kJoinUnits; ++q) {
+      for (int q = 0; q < NU; ++q) {
         if (u0 + q * 256 >= units) break;  // uniform
-        const int u = min(u0 + q * 256 + (int)threadIdx.x, units - 1);
+        const int u = min(u0 + q * 256 + t0, units - 1);
 #pragma unroll
-        for (int j = 0; j < kJoinSplits; ++j) {
-          const uint32_t row = parts.row(a, pc, min(s0 + j, pc.nsplit - 1), kvh, u / (kHD / 4));
+        for (int j = 0; j < NJ; ++j) {
+          const uint32_t row = parts.row(a, pc, min(s0 + j * groups, pc.nsplit - 1), kvh, u / (kHD / 4));
           ml[q][j] = coherent_load_f32x2(parts.ml, row * 8);
           ov[q][j] = coherent_load(parts.o, (row * kHD + (u % (kHD / 4)) * 4) * 4);
         }
       }
 #pragma unroll
-      for (int q = 0; q < kJoinUnits; ++q) {
+      for (int q = 0; q < NU; ++q) {
         if (u0 + q * 256 >= units) break;
         float mn = mx[q];
 #pragma unroll
-        for (int j = 0; j < kJoinSplits; ++j)
-          if (s0 + j < pc.nsplit) mn = fmaxf(mn, ml[q][j].x);
+        for (int j = 0; j < NJ; ++j)
+          if (s0 + j * groups < pc.nsplit) mn = fmaxf(mn, ml[q][j].x);
         // (a part without keys, or with nothing but NaN scores, has m = -inf: weight 0, and its NaN stays)
         const float f = mx[q] == -INFINITY ? 0.f : exp2f(mx[q] - mn);
         acc[q] *= f;
         sum[q] *= f;
         mx[q] = mn;
 #pragma unroll
-        for (int j = 0; j < kJoinSplits; ++j)
-          if (s0 + j < pc.nsplit) {
+        for (int j = 0; j < NJ; ++j)
+          if (s0 + j * groups < pc.nsplit) {
             const float w = ml[q][j].x == -INFINITY ? 0.f : exp2f(ml[q][j].x - mn);
             sum[q] += w * ml[q][j].y;
             acc[q] += w * ov[q][j];
           }
       }
     }
+    if (groups == 1) {
 #pragma unroll
-    for (int q = 0; q < kJoinUnits; ++q) {
-      const int u = u0 + q * 256 + (int)threadIdx.x;
-      if (u >= units) break;
-      const int r = u / (kHD / 4), d = (u % (kHD / 4)) * 4;
-      const float inv = 1.0f / sum[q];
-      bf16_t* dst = static_cast<bf16_t*>(a.out) + ((size_t)(pc.s.s0 + i0 + r / a.G) * a.H + kvh * a.G + r % a.G) * kHD + d;
-      *reinterpret_cast<u32x2*>(dst) = u32x2{pack_bf16x2(acc[q][0] * inv, acc[q][1] * inv), pack_bf16x2(acc[q][2] * inv, acc[q][3] * inv)};
+      for (int q = 0; q < NU; ++q)
+        if (u0 + q * 256 + t0 < units) write(u0 + q * 256 + t0, acc[q], sum[q]);
+    } else {
+      f32x4* s_acc = reinterpret_cast<f32x4*>(lds);
+      float2* s_ml = reinterpret_cast<float2*>(lds + 256 * 16);
+      s_acc[threadIdx.x] = acc[0];
+      s_ml[threadIdx.x] = float2{mx[0], sum[0]};
+      __syncthreads();
+      if (grp == 0) {
+        float mn = mx[0];
+        for (int g = 1; g < groups; ++g) mn = fmaxf(mn, s_ml[g * units + t0].x);
+        f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+        float l = 0.f;
+        for (int g = 0; g < groups; ++g) {
+          const float2 ml = s_ml[g * units + t0];
+          const float w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - mn);
+          l += w * ml.y;
+          o += w * s_acc[g * units + t0];
+        }
+        write(t0, o, l);
+      }
     }
   }
 }
@@ -480,7 +536,7 @@ __global__ __launch_bounds__(256, 2) void chunk_tile_kernel(ChunkAttnK a) {
   const int kvh = __builtin_amdgcn_readfirstlane(blockIdx.x % a.Hkv);
   if (blockIdx.x == 0) chunk_check(a.c);
   Piece pc;
-  if (!find_piece<kTiles>(a, blockIdx.x / a.Hkv, pc)) return;
+  if (!wg_piece<kTiles>(a, blockIdx.x / a.Hkv, pc)) return;
   const int G = a.G, tokens = a.tokens;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r32 = lane & 31, h = lane >> 5;
@@ -673,7 +729,7 @@ __global__ __launch_bounds__(256, 2) void chunk_tile_kernel(ChunkAttnK a) {
         parts.put(prow, 32 * dt + 8 * j + 4 * h, f32x4{o[dt][4 * j], o[dt][4 * j + 1], o[dt][4 * j + 2], o[dt][4 * j + 3]});
     if (h == 0) parts.put_ml(prow, m_run, l);
   }
-  if (pc.nsplit > 1) join_parts<kTiles>(a, pc, kvh, tokens, parts);
+  if (pc.nsplit > 1) join_parts<kTiles>(a, pc, kvh, tokens, parts, smem);
 }
 
 // ---------------------------------------------------------------------------
@@ -719,7 +775,7 @@ __global__ __launch_bounds__(256, 2) void chunk_stream_kernel(ChunkAttnK a) {
   const int kvh = __builtin_amdgcn_readfirstlane(blockIdx.x % a.Hkv);
   if (blockIdx.x == 0) chunk_check(a.c);
   Piece pc;
-  if (!find_piece<kStream>(a, blockIdx.x / a.Hkv, pc)) return;
+  if (!wg_piece<kStream>(a, blockIdx.x / a.Hkv, pc)) return;
   const int G = a.G, R = pc.s.n * G, len = pc.s.c + pc.s.n;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r16 = lane & 15, g = lane >> 4;
@@ -759,22 +815,21 @@ __global__ __launch_bounds__(256, 2) void chunk_stream_kernel(ChunkAttnK a) {
   };
   read_ids(0);
   bool odd = false;  // see redo_piece
+  // One step's fragments.  The next step's loads go out as soon as these are used,
+  // K under the softmax and the second product, V behind it (the order is pinned:
+  // hoisted loads would need registers of their own).  The wave's last step is
+  // code of its own: loads that may or may not have been issued would make the
+  // compiler wait for every load in flight, and loads past
+  // the end would all be of one page.
   u32x4 kr[8], vr[8], vsc;
   uint32_t ksc[NT];
-  int ids[NT];  // pages of the step whose K is loaded
-  // this lane's page of the step: of the token that it holds for K (block (W / 16 ..) of row m) and for V
-  auto pick = [&](int blk) {
-    int id = ids[0];
-#pragma unroll
-    for (int i = 1; i < NT; ++i) id = blk == i ? ids[i] : id;
-    return (size_t)max(id, 0) * a.Hkv + kvh;
-  };
+  size_t vhd = 0;  // (page, head) of the V to load
   const int ktok = W * (r16 >> 2) + (r16 & 3);  // token of score tile 0 (tile j: + 4 j, in the same block)
   auto load_k = [&](int j) {
     if (j - idbase >= kIds) read_ids(j);
-#pragma unroll
-    for (int i = 0; i < NT; ++i) ids[i] = __builtin_amdgcn_readlane(idv, NT * (j - idbase) + i);
-    const size_t hd = pick(ktok >> 4);
+    // this lane's blocks of the step: of its token for K, of its run for V
+    const size_t hd = (size_t)max(__shfl(idv, NT * (j - idbase) + (ktok >> 4)), 0) * a.Hkv + kvh;
+    vhd = (size_t)max(__shfl(idv, NT * (j - idbase) + (W * g >> 4)), 0) * a.Hkv + kvh;
     if constexpr (E4) {
       const char* src = static_cast<const char*>(a.kp) + (hd * kBlock + (ktok & 15)) * kHD + 16 * g;
 #pragma unroll
@@ -792,7 +847,7 @@ __global__ __launch_bounds__(256, 2) void chunk_stream_kernel(ChunkAttnK a) {
     }
   };
   auto load_v = [&]() {
-    const size_t hd = pick(W * g >> 4);
+    const size_t hd = vhd;
     const char* src = static_cast<const char*>(a.vp) +
                       (E4 ? (hd * kHD + r16) * kBlock : ((hd * kHD + r16) * kBlock + 8 * (g & 1)) * 2);
 #pragma unroll
@@ -808,11 +863,8 @@ __global__ __launch_bounds__(256, 2) void chunk_stream_kernel(ChunkAttnK a) {
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) o[t][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  if (n > 0) {
-    load_k(0);
-    load_v();
-  }
-  for (int j = 0; j < n; ++j) {
+  auto step = [&](auto lastc, int j) {
+    constexpr bool last = decltype(lastc)::value;
     f32x4 acc[RT][NT];
 #pragma unroll
     for (int t = 0; t < RT; ++t)
@@ -836,10 +888,12 @@ __global__ __launch_bounds__(256, 2) void chunk_stream_kernel(ChunkAttnK a) {
       if constexpr (E4) __builtin_amdgcn_sched_barrier(0);  // conversions hoisted further would need registers of their own
     }
     __builtin_amdgcn_sched_barrier(0);
-    if (j + 1 < n) load_k(j + 1);
+    if constexpr (!last) load_k(j + 1);
     __builtin_amdgcn_sched_barrier(0);
     const int t0 = k0 + ST * (wave + NP * j);
-    const bool masked = t0 + ST - 1 > pc.s.c || t0 + ST > k1;
+    // (a wave's steps are NP * ST >= 128 tokens apart and the rows see up to 32 tokens more or less: only its last
+    // step has anything to mask)
+    const bool masked = last && (t0 + ST - 1 > pc.s.c || t0 + ST > k1);
     float st[RT][W];
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
@@ -882,6 +936,7 @@ __global__ __launch_bounds__(256, 2) void chunk_stream_kernel(ChunkAttnK a) {
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             const int k = min(max(nv - 4 * c, 0), 4);
+            if (dt == 0) vsc[c] &= k == 4 ? 0xffffffffu : (1u << (8 * k)) - 1u;  // (any scale byte, 255 = infinity too)
             vr[dt][c] &= k == 4 ? 0xffffffffu : (1u << (8 * k)) - 1u;
             any |= (vr[dt][c] & 0x7f7f7f7fu) + 0x01010101u;  // a NaN code (magnitude 0x7f) carries into its top bit
           }
@@ -899,9 +954,7 @@ __global__ __launch_bounds__(256, 2) void chunk_stream_kernel(ChunkAttnK a) {
         if constexpr (E4) {
 #pragma unroll
           for (int e = 0; e < W; ++e) {
-            // (a masked token's slot may hold any scale byte: its probability stays 0)
-            const float sc = __uint_as_float(((vsc[e >> 2] >> (8 * (e & 3))) & 0xffu) << 23);
-            st[t][e] = st[t][e] == 0.f ? 0.f : st[t][e] * sc;
+            st[t][e] *= __uint_as_float(((vsc[e >> 2] >> (8 * (e & 3))) & 0xffu) << 23);
           }
         }
 #pragma unroll
@@ -924,15 +977,21 @@ __global__ __launch_bounds__(256, 2) void chunk_stream_kernel(ChunkAttnK a) {
       }
     }
     __builtin_amdgcn_sched_barrier(0);
-    if (j + 1 < n) load_v();
+    if constexpr (!last) load_v();
     __builtin_amdgcn_sched_barrier(0);
+  };
+  if (n > 0) {
+    load_k(0);
+    load_v();
+    for (int j = 0; j < n - 1; ++j) step(std::false_type{}, j);
+    step(std::true_type{}, n - 1);
   }
   if (__builtin_amdgcn_ballot_w64(bad) && lane == 0) flag_error(a.c.err, kErrBlock);
 
   const Parts<kStream> parts(a);
   if (__syncthreads_or(odd)) {
     redo_piece<PT, kStream>(a, pc, kvh, G, pc.s.n, k0, k1, reinterpret_cast<char*>(s_o), parts);
-    if (pc.nsplit > 1) join_parts<kStream>(a, pc, kvh, pc.s.n, parts);
+    if (pc.nsplit > 1) join_parts<kStream>(a, pc, kvh, pc.s.n, parts, reinterpret_cast<char*>(s_o));
     return;
   }
   // join the waves, then store the rows or this split's part
@@ -973,7 +1032,7 @@ __global__ __launch_bounds__(256, 2) void chunk_stream_kernel(ChunkAttnK a) {
       if (d == 0) parts.put_ml(prow, mx, sum);
     }
   }
-  if (pc.nsplit > 1) join_parts<kStream>(a, pc, kvh, pc.s.n, parts);
+  if (pc.nsplit > 1) join_parts<kStream>(a, pc, kvh, pc.s.n, parts, reinterpret_cast<char*>(s_o));
 }
 
 }  // namespace
@@ -1159,6 +1218,7 @@ int nightjar_chunk_attn(const nj_model_desc* desc, const nj_kv_layer* kv, const 
   a.D = d.head_dim;
   a.G = d.n_heads / d.n_kv_heads;
   a.tokens = kTileRows / a.G;
+  a.inv_tokens = a.tokens ? 1.0f / (float)a.tokens : 0.f;
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)d.head_dim);
   for (int k = 0; k < 2; ++k) {
     a.part_o[k] = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.o[k]);

@@ -142,6 +142,12 @@ def device_error(ws: Workspace, stream: Optional[int] = None) -> int:
     return nb.device_error(ws.ptr, ws.nbytes, s)
 
 
+def _current(t: torch.Tensor, stream: Optional[int]) -> int:
+    """The stream to enqueue on: the given one, or the current one of the tensor's device (without building a
+    torch.cuda.Stream, which takes longer than the rest of a call)."""
+    return torch._C._cuda_getCurrentRawStream(t.device.index) if stream is None else stream
+
+
 class KvLayer:
     """One layer's paged cache for the chunk calls: k [num_blocks][Hkv][16][D] and
     v [num_blocks][Hkv][D][16], fp32, bf16 (or its bits as int16), or e4m3 codes
@@ -223,7 +229,7 @@ def chunk_store(desc, layer: KvLayer, batch: ChunkBatch, qkv: torch.Tensor, ws: 
     _expect_layer(desc, layer)
     if q_out is not None:
         _expect_row(q_out, desc, batch.rows * desc.n_heads * desc.head_dim, "q_out")
-    s = torch.cuda.current_stream().cuda_stream if stream is None else stream
+    s = _current(qkv, stream)
     nb.chunk_store(desc, layer.c, batch.c, qkv.data_ptr(), qkv.stride(0) if batch.rows > 1 else width, _ptr(q_out),
                    ws.ptr, ws.nbytes, s)
 
@@ -234,7 +240,7 @@ def chunk_load(desc, layer: KvLayer, batch: ChunkBatch, k_out: torch.Tensor, v_o
     _expect_layer(desc, layer)
     for t, n in ((k_out, "k_out"), (v_out, "v_out")):
         _expect_row(t, desc, batch.rows * desc.n_kv_heads * desc.head_dim, n)
-    s = torch.cuda.current_stream().cuda_stream if stream is None else stream
+    s = _current(k_out, stream)
     nb.chunk_load(desc, layer.c, batch.c, k_out.data_ptr(), v_out.data_ptr(), ws.ptr, ws.nbytes, s)
 
 
@@ -244,7 +250,7 @@ def chunk_attn(desc, layer: KvLayer, batch: ChunkBatch, q: torch.Tensor, out: to
     _expect_layer(desc, layer)
     for t, n in ((q, "q"), (out, "out")):
         _expect_row(t, desc, batch.rows * desc.n_heads * desc.head_dim, n)
-    s = torch.cuda.current_stream().cuda_stream if stream is None else stream
+    s = _current(q, stream)
     nb.chunk_attn(desc, layer.c, batch.c, q.data_ptr(), out.data_ptr(), ws.ptr, ws.nbytes, s)
 
 
@@ -263,7 +269,7 @@ def sample(logits: torch.Tensor, uniforms: torch.Tensor, tokens: torch.Tensor, w
         _expect(t, torch.float32, R, n)
     _expect(tokens, torch.int32, R, "tokens")
     _expect(top_k, torch.int32, R, "top_k")
-    s = torch.cuda.current_stream().cuda_stream if stream is None else stream
+    s = _current(logits, stream)
     nb.sample(logits.data_ptr(), logits.stride(0) if R > 1 else V, R, V, _ptr(temperature), _ptr(top_k), _ptr(top_p),
               _ptr(min_p), _ptr(uniforms), _ptr(tokens), _ptr(probs), 0 if probs is None else probs.stride(0) if R > 1 else V,
               ws.ptr, ws.nbytes, s)
