@@ -27,7 +27,7 @@ struct ChunkAttnK {
   float scale_log2;
   int G, tokens;      // query heads per KV head, tokens of a tile (kTileRows / G)
   float inv_tokens;   // 1 / tokens
-  int cap[2];         // pieces per KV head up to which keys are cut, by class
+  int pieces[2];      // kPieces per KV head, by class (>= 1)
   int min_cut[2];     // shortest run of keys
   int threshold;      // sequences of more than this many query rows per KV head are cut into tiles, others streamed
   float* part_o[2];   // per class: [slot][rows of the class][kHD], unnormalised
@@ -39,18 +39,24 @@ struct ChunkAttnK {
 // Work.  A sequence's query rows for one KV head are its n tokens times the G
 // heads that share it, tokens first.  Class kTiles cuts them into tiles of up to
 // 128 rows (whole tokens), class kStream takes sequences of up to 32 rows whole.
-// When a class has fewer pieces than the chip takes, the keys of each piece are
-// cut too, into runs of at most L tokens, L the same for the whole class: with T
-// tiles that see W keys in all, runs of W / cap fit cap pieces if their ends
-// round well, and runs of W / (cap - T) always do.  The last part of a tile to be
-// done joins them.  Every workgroup works this out by itself from starts and
-// context lengths (one round of loads per 64 sequences, sums by DPP) instead of
+// Tiles that see many keys are cut along them, into runs of at most L tokens, L the
+// same for the whole class: its T tiles see W keys in all, and runs of W / kPieces fill
+// the chip (and even out lengths where T is large), but none is shorter than min_cut,
+// below which joining the parts costs more than it saves.  That makes at most
+// T + kPieces pieces, of which at most 2 kPieces belong to cut tiles.  The last part of
+// a tile to be done joins them.  Every workgroup works this out by itself from starts
+// and context lengths (one round of loads per 64 sequences, sums by DPP) instead of
 // reading a list that another kernel would have to write first.
 // ---------------------------------------------------------------------------
 enum { kTiles = 0, kStream = 1 };
 constexpr int kTileRows = 128, kStreamRows = 32;
-constexpr int kSlots[2] = {512, 1024};  // pieces (over all KV heads) up to which keys are cut
-constexpr int kMinCut[2] = {256, 128};  // tokens
+constexpr int kPieces[2] = {512, 512};  // over all KV heads: two workgroups a CU
+constexpr int kSlots[2] = {2 * kPieces[0], 2 * kPieces[1]};
+// Shortest runs, in tokens: of tiles, of streamed pieces of one row tile, and of two
+// (whose parts take longer to join).  One sequence of 1000 tokens, 4 rows: 10.6 us with
+// runs of 256, 12.5 of 512, 14.2 whole; 16 of 1024 tokens, 24 rows: 25.5, 26.0 and
+// 23.1 us.
+constexpr int kMinCutTiles = 256, kMinCutStream[2] = {256, 1024};
 
 struct Piece {
   ChunkSeq s;
@@ -71,16 +77,6 @@ __device__ __forceinline__ int wave_scan_i(int v) {
   return v;
 }
 __device__ __forceinline__ int wave_sum_i(int v) { return __builtin_amdgcn_readlane(wave_scan_i(v), 63); }
-__device__ __forceinline__ int wave_max_i(int v) {  // v >= 0
-  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));
-  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));
-  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));
-  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));
-  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));
-  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));
-  return __builtin_amdgcn_readlane(v, 63);
-}
-
 // ceil(x / L) for 0 <= x < 2^26 and L >= 1 with inv = 1 / L in fp32: the quotient is
 // off by one at most, which the products tell.
 __device__ __forceinline__ int ceil_div(int x, int L, float inv) {
@@ -98,9 +94,10 @@ __device__ __forceinline__ int class_tiles(const ChunkAttnK& a, const ChunkSeq& 
 // Piece `item` of class C (per KV head); false if there is none.  Run by one wave.
 template <int C>
 __device__ bool find_piece(const ChunkAttnK& a, int item, Piece& out) {
-  const int lane = threadIdx.x & 63, B = a.c.B, cap = a.cap[C];
-  // the class's tiles, the keys that they see (in units of 16, at most), and the longest range
-  int tiles = 0, keys = 0, longest = 0, t0 = 0;
+  const int lane = threadIdx.x & 63, B = a.c.B;
+  // the class's tiles and the keys that they see (in blocks of 16)
+  int tiles = 0, t0 = 0;
+  uint64_t keys = 0;
   ChunkSeq s0{0, 0, 0, false};
   for (int b0 = 0; b0 < B; b0 += kWave) {
     const int b = b0 + lane;
@@ -111,33 +108,19 @@ __device__ bool find_piece(const ChunkAttnK& a, int item, Piece& out) {
       t0 = t;
     }
     tiles += t;
-    keys += t * ((s.c + s.n + 15) >> 4);
-    longest = max(longest, t ? s.c + s.n : 0);
+    keys += (uint64_t)t * ((s.c + s.n + 15) >> 4);
   }
-  tiles = wave_sum_i(tiles);
-  if (tiles == 0) return false;
-  longest = wave_max_i(longest);
+  if (wave_sum_i(tiles) == 0) return false;
+  // (at most 2^24 tiles of 2^21 blocks in all: 64 bits)
+  const uint64_t all = ((uint64_t)(uint32_t)wave_sum_i((int)(keys >> 16)) << 16) + (uint32_t)wave_sum_i((int)(keys & 0xffff));
+  // (rounded up: L > W / pieces is what bounds the pieces)
+  const int L = max((int)fminf((float)all * (16.00002f / (float)a.pieces[C]) + 1.f, 0x1p30f), a.min_cut[C]);
   auto seq = [&](int b0, int& t) {
     const int b = b0 + lane;
     const ChunkSeq s = b0 == 0 ? s0 : b < B ? chunk_seq(a.c, b) : ChunkSeq{0, 0, 0, false};
     t = b0 == 0 ? t0 : class_tiles<C>(a, s);
     return s;
   };
-  int L = longest;
-  if (tiles * 2 <= cap && longest > kMinCut[C]) {
-    // (at most 2^9 tiles of 2^21 blocks: no sum leaves 32 bits)
-    keys = wave_sum_i(keys);
-    const auto cut = [&](int pieces) { return max((int)((int64_t)keys * 16 / pieces) + 1, a.min_cut[C]); };
-    L = cut(cap);
-    int cnt = 0;
-    const float inv = 1.0f / (float)L;
-    for (int b0 = 0; b0 < B; b0 += kWave) {
-      int t;
-      const ChunkSeq s = seq(b0, t);
-      cnt += t ? t * ceil_div(s.c + s.n, L, inv) : 0;
-    }
-    if (wave_sum_i(cnt) > cap) L = cut(cap - tiles);
-  }
   // the piece
   int before = 0, slots = 0;
   const float inv = 1.0f / (float)L;
@@ -766,7 +749,7 @@ __device__ __forceinline__ float quarter_max(float v) {
 
 constexpr int kMergeRow = kHD + 4;  // LDS row stride of the wave merge, in floats
 template <int PT, int RT>
-__global__ __launch_bounds__(256, 2) void chunk_stream_kernel(ChunkAttnK a) {
+__global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void chunk_stream_kernel(ChunkAttnK a) {
   constexpr bool E4 = PT == kPageE4M3;
   constexpr int NP = 4, ROWS = 16 * RT;
   constexpr int W = E4 ? 16 : 8, ST = 4 * W, NT = W / 4;  // tokens of a lane group and of a step, score tiles
@@ -1134,15 +1117,17 @@ hipError_t launch_chunk_attn(ChunkAttnK& a, const AttnParts& p, int pt, int B, i
   const bool all_long = p.tiles && (!p.stream || (int64_t)B * max_chunk <= rows);
   const bool one_tile = p.tiles || max_chunk * G <= 16;  // of the stream kernel's 16-row tiles
   a.threshold = all_long ? 0 : p.tiles ? 16 : INT_MAX;
+  a.min_cut[kTiles] = kMinCutTiles;
+  a.min_cut[kStream] = kMinCutStream[one_tile ? 0 : 1];
   hipError_t e = hipSuccess;
   if (p.tiles) {
-    const int pieces = std::max(rows / a.tokens + std::min(B, rows), a.cap[kTiles]);
+    const int pieces = rows / a.tokens + std::min(B, rows) + a.pieces[kTiles];
     hipLaunchKernelGGL(pt == kPageE4M3 ? chunk_tile_kernel<kPageE4M3> : chunk_tile_kernel<kPageBF16>, dim3(pieces * a.Hkv),
                        dim3(256), 0, s, a);
     e = hipGetLastError();
   }
   if (!all_long && e == hipSuccess) {
-    const int pieces = std::max(std::min(B, rows), a.cap[kStream]);
+    const int pieces = std::min(B, rows) + a.pieces[kStream];
     auto kern = pt == kPageE4M3 ? (one_tile ? chunk_stream_kernel<kPageE4M3, 1> : chunk_stream_kernel<kPageE4M3, 2>)
                                 : (one_tile ? chunk_stream_kernel<kPageBF16, 1> : chunk_stream_kernel<kPageBF16, 2>);
     hipLaunchKernelGGL(kern, dim3(pieces * a.Hkv), dim3(256), 0, s, a);
@@ -1224,8 +1209,7 @@ int nightjar_chunk_attn(const nj_model_desc* desc, const nj_kv_layer* kv, const 
     a.part_o[k] = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.o[k]);
     a.part_ml[k] = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.ml[k]);
     a.counters[k] = reinterpret_cast<int*>(static_cast<char*>(workspace) + p.cnt[k]);
-    a.cap[k] = kSlots[k] / d.n_kv_heads;
-    a.min_cut[k] = kMinCut[k];
+    a.pieces[k] = std::max(1, kPieces[k] / d.n_kv_heads);
   }
   const hipError_t e = launch_chunk_attn(a, p, page_type(kv), batch->B, batch->rows, batch->max_chunk, (hipStream_t)stream);
   return e == hipSuccess ? NJ_OK : set_last_error(NJ_EHIP, "chunk_attn: %s", hipGetErrorString(e));
