@@ -199,16 +199,30 @@ __device__ __forceinline__ float half_max(float v) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
+// Max of 8, 16 or 32 values, three operands at a time (NaN is dropped, as by fmaxf).
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+__device__ __forceinline__ float max_of(const float (&v)[8]) {
+  return max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), fmaxf(v[6], v[7]));
+}
+__device__ __forceinline__ float max_of(const float (&v)[16]) {
+  return max3(max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), max3(v[6], v[7], v[8])),
+              max3(max3(v[9], v[10], v[11]), max3(v[12], v[13], v[14]), v[15]), v[15]);
+}
+
+__device__ __forceinline__ float max_of(const float (&v)[32]) {
+  float m[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) m[i] = fmaxf(v[2 * i], v[2 * i + 1]);
+  return max_of(m);
+}
+
 // One online-softmax step over N scores of a lane's query row (-inf where
 // masked): reference = the row's max, so that a leading token's probability is
 // exactly 1 in bf16; the accumulators are rescaled only when some row's max rose.
 // Scores become probabilities relative to 2^m_run.
 template <int N>
 __device__ __forceinline__ void softmax_step(float (&st)[N], float scale, float& m_run, float& l_run, f32x16 (&o)[4]) {
-  float mx[4] = {st[0], st[1], st[2], st[3]};
-#pragma unroll
-  for (int i = 4; i < N; ++i) mx[i & 3] = fmaxf(mx[i & 3], st[i]);
-  const float bm = half_max(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]))) * scale;
+  const float bm = half_max(max_of(st)) * scale;
   const bool rises = bm > m_run;
   if (__builtin_amdgcn_ballot_w64(rises)) {
     const float mn = rises ? bm : m_run;
@@ -242,12 +256,15 @@ __device__ __forceinline__ bf16x8 keep_tokens(bf16x8 v, int nv) {
   for (int e = 0; e < 4; ++e) w[e] &= nv >= 2 * e + 2 ? 0xffffffffu : nv == 2 * e + 1 ? 0xffffu : 0u;
   return __builtin_bit_cast(bf16x8, w);
 }
-__device__ __forceinline__ bool has_nonfinite(bf16x8 v) {
+// Nonzero in bits 15 or 31 where a fragment holds a NaN or an infinity: an exponent
+// of all ones carries into the sign's place.
+constexpr uint32_t kNonfiniteBits = 0x80008000u;
+__device__ __forceinline__ uint32_t nonfinite_bits(bf16x8 v) {
   const u32x4 w = __builtin_bit_cast(u32x4, v);
-  bool bad = false;
+  uint32_t any = 0;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) bad |= (w[e] & 0x7f80u) == 0x7f80u || (w[e] & 0x7f800000u) == 0x7f800000u;
-  return bad;
+  for (int e = 0; e < 4; ++e) any |= (w[e] & 0x7f807f80u) + 0x00800080u;
+  return any;
 }
 
 // Element i of an array of page type PT (e4m3: the code's value, without its scale).
@@ -527,12 +544,11 @@ __global__ __launch_bounds__(256, 2) void chunk_tile_kernel(ChunkAttnK a) {
   int k0, k1;
   split_range(len, pc.split, pc.nsplit, k0, k1);
 
-  // this lane's query row, its last visible key, and the wave's first and last
+  // this lane's query row, its last visible key, and the wave's last
   const int r = wave * 32 + r32, i = i0 + r / G, head = kvh * G + r % G;
   const bool row_ok = r < tokens * G && i < pc.s.n;
   const int ic = min(i, pc.s.n - 1), vis = pc.s.c + ic;
   const int row = pc.s.s0 + ic;
-  const int vis_lo = pc.s.c + __builtin_amdgcn_readfirstlane(min(i0 + wave * 32 / G, pc.s.n - 1));
   const int vis_hi = pc.s.c + __builtin_amdgcn_readfirstlane(min(i0 + (wave * 32 + 31) / G, pc.s.n - 1));
   const bool wave_on = wave * 32 < tokens * G && i0 + wave * 32 / G < pc.s.n;
   bf16x8 qf[8];
@@ -548,7 +564,7 @@ __global__ __launch_bounds__(256, 2) void chunk_tile_kernel(ChunkAttnK a) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[dt][e] = 0.f;
 
-  bool odd = false;  // see redo_piece
+  uint32_t odd = 0;  // kNonfiniteBits: see redo_piece
   const int nit = (k1 - k0 + kStep - 1) / kStep;
   // page ids of this wave's block of 64 stages (lane l: stage idbase + l); bad
   // ones and blocks behind the last key read page 0, whose tokens are masked (or,
@@ -643,63 +659,84 @@ __global__ __launch_bounds__(256, 2) void chunk_tile_kernel(ChunkAttnK a) {
   const int kaddr = (mt >> 4) * kBlkBytes + (mt & 15) * 256 + ((h ^ (mt & 15)) * 16);
   const int vaddr = kStageBytes / 2 + r32 * 32 + ((h ^ (r32 >> 4)) * 16);
 
+  // One stage's products: both score products, one softmax step over the 64 tokens
+  // (one rescale test), and behind it the second products, among which the compiler
+  // spreads the exponentials.  V's first fragments are read under the softmax.
+  auto stage = [&](auto maskedc, int it) {
+    constexpr bool masked = decltype(maskedc)::value;
+    const char* buf = smem + (it & 1) * kStageBytes;
+    const int t0 = k0 + it * kStep;
+    f32x16 acc[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[x][e] = 0.f;
+#pragma unroll
+      for (int s = 0; s < 8; ++s)
+        acc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld8(buf + ((kaddr ^ (32 * s)) + x * 2 * kBlkBytes)), qf[s], acc[x], 0, 0, 0);
+    }
+    bf16x8 vf[4];
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) vf[dt] = ld8(buf + vaddr + dt * 1024);
+    float st[32];
+#pragma unroll
+    for (int e = 0; e < 32; ++e) st[e] = acc[e >> 4][e & 15];
+    if constexpr (masked) {
+      const int lim = min(vis, k1 - 1) - t0;
+#pragma unroll
+      for (int e = 0; e < 32; ++e) st[e] = 16 * (e >> 3) + 8 * h + (e & 7) <= lim ? st[e] : -INFINITY;
+    }
+    softmax_step(st, a.scale_log2, m_run, l_run, o);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const bf16x8 pf = pack8(st + 8 * x);
+      bf16x8 vn[4];
+      if (x < 3) {
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) vn[dt] = ld8(buf + vaddr + (x + 1) * kBlkBytes + dt * 1024);
+      }
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt) {
+        if constexpr (masked) {  // a masked token's V must not be NaN or infinite: 0 times it would not be 0
+          vf[dt] = keep_tokens(vf[dt], k1 - t0 - 16 * x - 8 * h);
+          odd |= nonfinite_bits(vf[dt]);
+        }
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[dt], pf, o[dt], 0, 0, 0);
+      }
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt) vf[dt] = vn[dt];
+    }
+  };
+  auto next = [&](int it) {
+    // this stage is in LDS, and every wave is done with the buffer that the next one goes to
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (it + 1 < nit) load(it + 1);
+  };
   if (nit > 0) {
     read_ids(0);
     load(0);
     convert(0);
   }
-  for (int it = 0; it < nit; ++it) {
-    // this stage is in LDS (loads of the compiler's own are waited for with it), and every wave is done with the
-    // buffer that the next one goes to
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (it + 1 < nit) load(it + 1);
-    const char* buf = smem + (it & 1) * kStageBytes;
-    const int t0 = k0 + it * kStep;
-    if (wave_on && t0 <= vis_hi) {
-      f32x16 acc[2];
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc[x][e] = 0.f;
-#pragma unroll
-        for (int s = 0; s < 8; ++s)
-          acc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld8(buf + ((kaddr ^ (32 * s)) + x * 2 * kBlkBytes)), qf[s], acc[x], 0, 0, 0);
-      }
-      float st[32];
-#pragma unroll
-      for (int e = 0; e < 32; ++e) st[e] = acc[e >> 4][e & 15];
-      const bool masked = t0 + kStep - 1 > vis_lo || t0 + kStep > k1;
-      const int lim = min(vis, k1 - 1) - t0;
-      if (masked) {
-#pragma unroll
-        for (int e = 0; e < 32; ++e) st[e] = 16 * (e >> 3) + 8 * h + (e & 7) <= lim ? st[e] : -INFINITY;
-      }
-      softmax_step(st, a.scale_log2, m_run, l_run, o);
-      if (masked) {  // a masked token's V must not be NaN or infinite: 0 times it would not be 0
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-#pragma unroll
-          for (int dt = 0; dt < 4; ++dt)
-            odd |= has_nonfinite(keep_tokens(ld8(buf + vaddr + x * kBlkBytes + dt * 1024), k1 - t0 - 16 * x - 8 * h));
-      }
-      const bool tail = t0 + kStep > k1;
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const bf16x8 pf = pack8(st + 8 * x);
-#pragma unroll
-        for (int dt = 0; dt < 4; ++dt) {
-          bf16x8 vf = ld8(buf + vaddr + x * kBlkBytes + dt * 1024);
-          if (tail) vf = keep_tokens(vf, k1 - t0 - 16 * x - 8 * h);
-          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[dt], 0, 0, 0);
-        }
-      }
-    }
+  // no load of the compiler's own is left for the loop to wait for: it would wait for the stage loads with it
+  __builtin_amdgcn_s_waitcnt(0x0f70);
+  // Stages that every row of the tile sees whole come first, in a loop without masks (as selects they took a third
+  // of the vector work).
+  const int vis0 = pc.s.c + i0;  // the first row's last key
+  const int full = min(max((min(vis0 + 1, k1) - k0) / kStep, 0), nit);
+  for (int it = 0; it < full; ++it) {
+    next(it);
+    if (wave_on) stage(std::false_type{}, it);
+    if (it + 1 < nit) convert(it + 1);
+  }
+  for (int it = full; it < nit; ++it) {
+    next(it);
+    if (wave_on && k0 + it * kStep <= vis_hi) stage(std::true_type{}, it);
     if (it + 1 < nit) convert(it + 1);
   }
   if (__builtin_amdgcn_ballot_w64(bad) && lane == 0) flag_error(a.c.err, kErrBlock);
   const Parts<kTiles> parts(a);
   const float l = l_run + __shfl_xor(l_run, 32);
-  if (__syncthreads_or(odd)) {
+  if (__syncthreads_or((odd & kNonfiniteBits) != 0)) {
     redo_piece<PT, kTiles>(a, pc, kvh, G, tokens, k0, k1, smem, parts);
   } else if (pc.nsplit == 1) {
     if (row_ok) store_row(a, row, head, o, 1.0f / l);
@@ -797,7 +834,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void chunk_stream_kernel(Chun
     idv = id;
   };
   read_ids(0);
-  bool odd = false;  // see redo_piece
+  uint32_t odd = 0;  // kNonfiniteBits: see redo_piece
   // One step's fragments.  The next step's loads go out as soon as these are used,
   // K under the softmax and the second product, V behind it (the order is pinned:
   // hoisted loads would need registers of their own).  The wave's last step is
@@ -888,10 +925,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void chunk_stream_kernel(Chun
         for (int e = 0; e < W; ++e) st[t][e] = e <= lim ? st[t][e] : -INFINITY;
       }
       // online softmax, reference = the row's max (see softmax_step)
-      float mx[4] = {st[t][0], st[t][1], st[t][2], st[t][3]};
-#pragma unroll
-      for (int e = 4; e < W; ++e) mx[e & 3] = fmaxf(mx[e & 3], st[t][e]);
-      const float bm = quarter_max(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]))) * a.scale_log2;
+      const float bm = quarter_max(max_of(st[t])) * a.scale_log2;
       const bool rises = bm > m_run[t];
       if (__builtin_amdgcn_ballot_w64(rises)) {
         const float mn = rises ? bm : m_run[t];
@@ -923,11 +957,11 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void chunk_stream_kernel(Chun
             vr[dt][c] &= k == 4 ? 0xffffffffu : (1u << (8 * k)) - 1u;
             any |= (vr[dt][c] & 0x7f7f7f7fu) + 0x01010101u;  // a NaN code (magnitude 0x7f) carries into its top bit
           }
-          odd |= (any & 0x80808080u) != 0;
+          odd |= any & 0x80808080u ? kNonfiniteBits : 0;
         } else {
           const bf16x8 v = keep_tokens(__builtin_bit_cast(bf16x8, vr[dt]), nv);
           vr[dt] = __builtin_bit_cast(u32x4, v);
-          odd |= has_nonfinite(v);
+          odd |= nonfinite_bits(v);
         }
       }
     }
@@ -972,7 +1006,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void chunk_stream_kernel(Chun
   if (__builtin_amdgcn_ballot_w64(bad) && lane == 0) flag_error(a.c.err, kErrBlock);
 
   const Parts<kStream> parts(a);
-  if (__syncthreads_or(odd)) {
+  if (__syncthreads_or((odd & kNonfiniteBits) != 0)) {
     redo_piece<PT, kStream>(a, pc, kvh, G, pc.s.n, k0, k1, reinterpret_cast<char*>(s_o), parts);
     if (pc.nsplit > 1) join_parts<kStream>(a, pc, kvh, pc.s.n, parts, reinterpret_cast<char*>(s_o));
     return;
