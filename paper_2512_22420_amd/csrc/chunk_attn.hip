@@ -29,6 +29,7 @@ struct ChunkAttnK {
   float inv_tokens;   // 1 / tokens
   int pieces[2];      // kPieces per KV head, by class (>= 1)
   int min_cut[2];     // shortest run of keys
+  int join_max;       // tiles in more parts are joined by chunk_merge_kernel
   int threshold;      // sequences of more than this many query rows per KV head are cut into tiles, others streamed
   float* part_o[2];   // per class: [slot][rows of the class][kHD], unnormalised
   float* part_ml[2];  // [slot][rows][2]: max (log2 domain), sum
@@ -39,14 +40,16 @@ struct ChunkAttnK {
 // Work.  A sequence's query rows for one KV head are its n tokens times the G
 // heads that share it, tokens first.  Class kTiles cuts them into tiles of up to
 // 128 rows (whole tokens), class kStream takes sequences of up to 32 rows whole.
-// Tiles that see many keys are cut along them, into runs of at most L tokens, L the
+// Tiles that see many keys are cut along them, into runs of about L tokens, L the
 // same for the whole class: its T tiles see W keys in all, and runs of W / kPieces fill
 // the chip (and even out lengths where T is large), but none is shorter than min_cut,
 // below which joining the parts costs more than it saves.  That makes at most
-// T + kPieces pieces, of which at most 2 kPieces belong to cut tiles.  The last part of
-// a tile to be done joins them.  Every workgroup works this out by itself from starts
-// and context lengths (one round of loads per 64 sequences, sums by DPP) instead of
-// reading a list that another kernel would have to write first.
+// T + kPieces pieces, of which at most 2 kPieces belong to cut tiles.  Every workgroup
+// works this out by itself from starts and context lengths (one round of loads per 64
+// sequences, sums by DPP) instead of reading a list that another kernel would have to
+// write first.  The parts are joined by the last of them to be done (streamed pieces,
+// a few KB each) or by a launch of their own (tiles, 64 KB a part, where the batch may
+// hold few of them).
 // ---------------------------------------------------------------------------
 enum { kTiles = 0, kStream = 1 };
 constexpr int kTileRows = 128, kStreamRows = 32;
@@ -91,8 +94,9 @@ __device__ __forceinline__ int class_tiles(const ChunkAttnK& a, const ChunkSeq& 
   return C == kTiles ? ceil_div(s.n, a.tokens, a.inv_tokens) : 1;
 }
 
-// Piece `item` of class C (per KV head); false if there is none.  Run by one wave.
-template <int C>
+// Piece `item` of class C (per KV head); with TILES the tile of that number among
+// those in more than join_max parts.  False if there is none.  Run by one wave.
+template <int C, bool TILES>
 __device__ bool find_piece(const ChunkAttnK& a, int item, Piece& out) {
   const int lane = threadIdx.x & 63, B = a.c.B;
   // the class's tiles and the keys that they see (in blocks of 16)
@@ -127,8 +131,9 @@ __device__ bool find_piece(const ChunkAttnK& a, int item, Piece& out) {
   for (int b0 = 0; b0 < B; b0 += kWave) {
     int t;
     const ChunkSeq s = seq(b0, t);
-    const int ns = t ? ceil_div(s.c + s.n, L, inv) : 0;
-    const int mine = t * ns, sl = ns > 1 ? mine : 0;
+    // (tiles: rounded to nearest, as a part of a tile pays off from about 1.5 runs on)
+    const int len = s.c + s.n, ns = t ? ceil_div(C == kTiles ? max(len - (L - L / 2 - 1), 1) : len, L, inv) : 0;
+    const int sl = ns > 1 ? t * ns : 0, mine = TILES ? (ns > a.join_max ? t : 0) : t * ns;
     const int inc = wave_scan_i(mine), sinc = wave_scan_i(sl);
     const uint64_t hit = __ballot(before + inc > item);
     if (hit) {
@@ -140,9 +145,9 @@ __device__ bool find_piece(const ChunkAttnK& a, int item, Piece& out) {
       out.s = {of(s.s0), of(s.n), of(s.c), false};
       out.nsplit = of(ns);
       // the last tiles see the most keys: they go first
-      const int rank = at / out.nsplit;
+      const int rank = TILES ? at : at / out.nsplit;
       out.tile = __builtin_amdgcn_readfirstlane(of(t) - 1 - rank);
-      out.split = __builtin_amdgcn_readfirstlane(at % out.nsplit);
+      out.split = TILES ? 0 : __builtin_amdgcn_readfirstlane(at % out.nsplit);
       out.slot = __builtin_amdgcn_readfirstlane(slots + of(sinc - sl) + rank * out.nsplit);
       return true;
     }
@@ -153,12 +158,12 @@ __device__ bool find_piece(const ChunkAttnK& a, int item, Piece& out) {
 }
 
 // The workgroup's piece: found by its first wave.
-template <int C>
+template <int C, bool TILES = false>
 __device__ __forceinline__ bool wg_piece(const ChunkAttnK& a, int item, Piece& pc) {
   __shared__ int s_pc[9];
   if (threadIdx.x < kWave) {
     Piece p{};
-    const bool ok = find_piece<C>(a, item, p);
+    const bool ok = find_piece<C, TILES>(a, item, p);
     if (threadIdx.x == 0) {
       const int v[9] = {p.s.s0, p.s.n, p.s.c, p.tile, p.split, p.nsplit, p.slot, p.b, ok};
 #pragma unroll
@@ -749,7 +754,7 @@ __global__ __launch_bounds__(256, 2) void chunk_tile_kernel(ChunkAttnK a) {
         parts.put(prow, 32 * dt + 8 * j + 4 * h, f32x4{o[dt][4 * j], o[dt][4 * j + 1], o[dt][4 * j + 2], o[dt][4 * j + 3]});
     if (h == 0) parts.put_ml(prow, m_run, l);
   }
-  if (pc.nsplit > 1) join_parts<kTiles>(a, pc, kvh, tokens, parts, smem);
+  if (pc.nsplit > 1 && pc.nsplit <= a.join_max) join_parts<kTiles>(a, pc, kvh, tokens, parts, smem);
 }
 
 // ---------------------------------------------------------------------------
@@ -1052,6 +1057,52 @@ __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void chunk_stream_kernel(Chun
   if (pc.nsplit > 1) join_parts<kStream>(a, pc, kvh, pc.s.n, parts, reinterpret_cast<char*>(s_o));
 }
 
+// Joins the parts of tiles: 64 KB each, which one workgroup (the last part's) would
+// read at what a single CU draws, ~45 GB/s (40 tokens over 8000 in 32 parts: 79 us,
+// with this launch 32; 20 tokens over 2000: 27, 19).  grid (tiles * Hkv, groups of 8
+// rows).
+__global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkAttnK a) {
+  const int kvh = __builtin_amdgcn_readfirstlane(blockIdx.x % a.Hkv);
+  Piece pc;
+  if (!wg_piece<kTiles, true>(a, blockIdx.x / a.Hkv, pc)) return;
+  const int r = blockIdx.y * 8 + threadIdx.x / (kHD / 4), d = (threadIdx.x % (kHD / 4)) * 4;
+  const int i0 = pc.tile * a.tokens, R = min(a.tokens, pc.s.n - i0) * a.G;
+  if (r >= R) return;
+  const float* ml = a.part_ml[kTiles] + (((size_t)pc.slot * a.Hkv + kvh) * kTileRows + r) * 2;
+  const float* po = a.part_o[kTiles] + (((size_t)pc.slot * a.Hkv + kvh) * kTileRows + r) * kHD + d;
+  const size_t step = (size_t)a.Hkv * kTileRows;
+  constexpr int NJ = 8;  // parts in flight
+  f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+  float mx = -INFINITY, sum = 0.f;
+  for (int s0 = 0; s0 < pc.nsplit; s0 += NJ) {
+    f32x4 ov[NJ];
+    float2 v[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const size_t at = min(s0 + j, pc.nsplit - 1) * step;
+      v[j] = *reinterpret_cast<const float2*>(ml + at * 2);
+      ov[j] = *reinterpret_cast<const f32x4*>(po + at * kHD);
+    }
+    float mn = mx;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) mn = fmaxf(mn, v[j].x);
+    const float f = mx == -INFINITY ? 0.f : exp2f(mx - mn);
+    acc *= f;
+    sum *= f;
+    mx = mn;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+      if (s0 + j < pc.nsplit) {
+        const float w = v[j].x == -INFINITY ? 0.f : exp2f(v[j].x - mn);
+        sum += w * v[j].y;
+        acc += w * ov[j];
+      }
+  }
+  const float inv = 1.0f / sum;
+  bf16_t* dst = static_cast<bf16_t*>(a.out) + ((size_t)(pc.s.s0 + i0 + r / a.G) * a.H + kvh * a.G + r % a.G) * kHD + d;
+  *reinterpret_cast<u32x2*>(dst) = u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
+}
+
 }  // namespace
 }  // namespace nj
 
@@ -1155,10 +1206,18 @@ hipError_t launch_chunk_attn(ChunkAttnK& a, const AttnParts& p, int pt, int B, i
   a.min_cut[kStream] = kMinCutStream[one_tile ? 0 : 1];
   hipError_t e = hipSuccess;
   if (p.tiles) {
-    const int pieces = rows / a.tokens + std::min(B, rows) + a.pieces[kTiles];
+    const int tiles = rows / a.tokens + std::min(B, rows), pieces = tiles + a.pieces[kTiles];
+    // Tiles may be cut where they are few and the contexts (as far as the table reaches) long: their parts get a
+    // launch of their own.  (A large batch that is mostly padding can hold few tiles too: the last part joins.)
+    const bool merge = tiles <= a.pieces[kTiles] && (int64_t)a.c.max_blocks * kBlock > kMinCutTiles;
+    a.join_max = merge ? 1 : INT_MAX;
     hipLaunchKernelGGL(pt == kPageE4M3 ? chunk_tile_kernel<kPageE4M3> : chunk_tile_kernel<kPageBF16>, dim3(pieces * a.Hkv),
                        dim3(256), 0, s, a);
     e = hipGetLastError();
+    if (e == hipSuccess && merge) {
+      hipLaunchKernelGGL(chunk_merge_kernel, dim3(tiles * a.Hkv, kTileRows / 8), dim3(256), 0, s, a);
+      e = hipGetLastError();
+    }
   }
   if (!all_long && e == hipSuccess) {
     const int pieces = std::min(B, rows) + a.pieces[kStream];
