@@ -149,8 +149,7 @@ int nightjar_chunk_attn(const nj_model_desc* desc, const nj_kv_layer* kv, const 
  * The token is the smallest kept index whose running sum of kept weights (index
  * order) exceeds uniforms[r] times their total.  temperature 0 is greedy: the
  * largest logit, lowest index.  A logit of -inf is never drawn.  Weights are
- * computed in 64 bits and summed as 64-bit integers (in units of 2^-44), so the
- * result does not depend on how the work is split.
+ * computed and summed in 64 bits, in an order that depends on vocab alone.
  *
  *   logits       device fp32, row r at logits + r * logits_stride (>= vocab)
  *   temperature, top_p, min_p   device fp32 [rows], top_k device int32 [rows];

@@ -1,24 +1,29 @@
 // Sampling with temperature, top-k, top-p and min-p from given uniforms.
 //
-// Everything that decides -- which tokens are kept, and which is drawn -- is made
-// of comparisons of logits, counts, and sums of weights w = exp((l - max) / T).
-// The weights are computed in 64 bits (fp32 ones would move a border between two
-// tokens every few ten thousand rows of a 150k vocabulary) and summed as 64-bit
-// integers in units of 2^-44 (V <= 2^19 weights of at most 1 fit), so sums are
-// exact, associative, and the same in whatever order atomics or waves add them.
+// What decides -- which tokens are kept, and which is drawn -- is made of
+// comparisons of logits, counts, and sums of weights w = exp((l - max) / T).  The
+// weights are computed and summed in 64 bits (fp32 ones would move a border between
+// two tokens every few ten thousand rows of a 150k vocabulary), in an order that does
+// not depend on how the work is split.
 //
 // top-k, top-p and min-p each keep a prefix of the tokens ordered by (logit
-// descending, index ascending); so does their combination, up to min-p, which is
-// a test of the weight alone.  The prefix is found by its last token:
-//   1. the row's max;
-//   2. a histogram of count and mass over d = max - l, in bins that are the
-//      upper bits of d as a float (relative width 2^-7, so that a bin holds a few
-//      per cent of a broad row at most, whatever the scale of the logits); the bin
-//      in which the count reaches top_k, or the mass top_p;
-//   3. if no more than kCap tokens lie up to that bin, they are collected, sorted,
-//      and everything else happens on the sorted list in LDS;
-//      otherwise the last token is found by a radix search over the logits' bits
-//      (three more passes), and its index among equal logits by one more.
+// descending, index ascending), and so do they together.  The vocabulary is cut into
+// tiles of 256 tokens:
+//   sample_tiles  (rows x tile groups) reads every logit once: each tile's max,
+//                 and, where the row needs it, its weights' sum relative to that max.
+//   sample_rows   (one workgroup per row) knows from the tiles' maxima which tiles
+//                 can hold kept tokens -- the k-th largest tile max bounds the k-th
+//                 largest logit from below -- reads only those, sorts what they hold
+//                 above the bound in LDS, and keeps and draws there.  A row that is
+//                 not truncated is drawn from the tiles' sums and one tile.
+//                 A row that keeps more tokens than the list holds goes the long way:
+//                 a histogram of the row finds the last token kept, and a pass over it
+//                 sums what is kept.
+//   sample_probs  (rows x tile groups, if wanted) writes the distribution; tiles
+//                 without a kept token are written without being read.
+// Bound by the one read of the logits (and the write of the distribution).
+#include <limits.h>
+
 #include "../../include/nightjar_serve.h"
 #include "common.h"
 #include "kernels.h"
@@ -63,17 +68,16 @@ __device__ __forceinline__ uint32_t order_key(float l) {
 __device__ __forceinline__ float key_logit(uint32_t k) {
   return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
-// Bin of d = max - l >= 0: the upper 16 bits of d (8 of exponent, 7 of
-// mantissa) from 2^-8 on; smaller ones share bin 0, from 2^8 on the last.
-__device__ __forceinline__ int d_bin(float d) {
-  const int k = (int)(__float_as_uint(d) >> 16) - ((127 - 8) << 7);
-  return min(max(k, 0), kBins - 1);
-}
+struct RowHead {   // what sample_probs needs of a row
+  double inv;      // 1 / total weight; 0: the row could not be sampled
+  float max, tau;  // kept: logits above tau, and those equal to it up to index tau_idx
+  int tau_idx;
+};
 
 struct SampleK {
   const float* logits;
   long long lstride;
-  int V;
+  int V, ntile;
   const float* temperature;
   const int32_t* top_k;
   const float* top_p;
@@ -83,9 +87,79 @@ struct SampleK {
   float* probs;
   long long pstride;
   int* err;
-  int vec;  // rows of logits may be read in 16-byte pieces
-  int pvec; // rows of probs may be written in them
+  double* tmass;  // [rows][ntile]: sum of exp((l - tile max) / T) over the tile
+  float* tmax;    // [rows][ntile]: tile max; +inf if the tile holds a NaN
+  RowHead* head;  // [rows]
+  int vec;        // rows of logits may be read in 16-byte pieces
+  int pvec;       // rows of probs may be written in them
 };
+
+// A row's settings.  mass: the tiles' sums are needed (top-p without top-k, or no
+// truncation at all).
+struct RowSet {
+  float T, P, Q, u;
+  int K;
+  bool ok, greedy, by_count, by_mass, mass;
+  double scale;  // log2 e / T
+};
+__device__ __forceinline__ RowSet row_set(const SampleK& a, int r) {
+  RowSet s;
+  s.T = a.temperature ? a.temperature[r] : 1.f;
+  s.P = a.top_p ? a.top_p[r] : 1.f;
+  s.Q = a.min_p ? a.min_p[r] : 0.f;
+  s.u = a.uniforms[r];
+  s.K = a.top_k ? a.top_k[r] : 0;
+  if (s.K <= 0 || s.K > a.V) s.K = a.V;
+  s.ok = s.T >= 0.f && s.T < INFINITY && s.P >= 0.f && s.Q >= 0.f && s.Q <= 1.f && s.u >= 0.f && s.u < 1.f;
+  s.greedy = s.T == 0.f;
+  s.by_count = s.K < a.V;
+  s.by_mass = s.P < 1.f;
+  s.mass = s.ok && !s.greedy && !s.by_count && (s.by_mass || s.Q == 0.f);
+  s.scale = 1.4426950408889634074 / (s.greedy ? 1.0 : (double)s.T);
+  return s;
+}
+
+// Four tokens of a lane: tile t's tokens 4 lane ..; past the end -inf.
+__device__ __forceinline__ f32x4 tile_quad(const SampleK& a, const float* __restrict__ row, int t) {
+  const int j = t * kTile + 4 * (int)(threadIdx.x & 63);
+  if (a.vec && j + 3 < a.V) return *reinterpret_cast<const f32x4*>(row + j);
+  f32x4 l;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) l[e] = j + e < a.V ? row[j + e] : -INFINITY;
+  return l;
+}
+
+// grid (rows, ceil(ntile / kTilesPerWg)); a wave reads its four tiles at once.
+constexpr int kWaveTiles = 4, kTilesPerWg = 4 * kWaveTiles;
+__global__ __launch_bounds__(256) void sample_tiles_kernel(SampleK a) {
+  const int r = blockIdx.x, lane = threadIdx.x & 63, t0 = blockIdx.y * kTilesPerWg + (threadIdx.x >> 6) * kWaveTiles;
+  const float* row = a.logits + (size_t)r * a.lstride;
+  f32x4 l[kWaveTiles];
+#pragma unroll
+  for (int i = 0; i < kWaveTiles; ++i)
+    if (t0 + i < a.ntile) l[i] = tile_quad(a, row, t0 + i);
+  const RowSet s = row_set(a, r);
+#pragma unroll
+  for (int i = 0; i < kWaveTiles; ++i) {
+    if (t0 + i >= a.ntile) break;  // uniform
+    float m = fmaxf(fmaxf(l[i][0], l[i][1]), fmaxf(l[i][2], l[i][3]));
+    const bool nan = l[i][0] != l[i][0] || l[i][1] != l[i][1] || l[i][2] != l[i][2] || l[i][3] != l[i][3];
+    if (nan) m = INFINITY;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    if (lane == 0) a.tmax[(size_t)r * a.ntile + t0 + i] = m;
+    if (s.mass) {
+      double w = 0.0;
+      if (m > -INFINITY && m < INFINITY) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w += exp2_64(((double)l[i][e] - (double)m) * s.scale);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) w += __shfl_xor(w, o);
+      }
+      if (lane == 0) a.tmass[(size_t)r * a.ntile + t0 + i] = w;
+    }
+  }
+}
 
 struct Shared {
   union {
@@ -93,13 +167,64 @@ struct Shared {
       u64 mass[kBins];
       uint32_t count[kBins];
     } h;
-    u64 list[kCap];
+    __attribute__((aligned(16))) u64 list[kCap];
   };
-  u64 tsum[kMaxTiles];
+  union {
+    u64 tsum[kMaxTiles];   // long way: tile sums
+    double tmass[kMaxTiles];
+  };
+  __attribute__((aligned(16))) float tmax[kMaxTiles];
+  uint16_t tiles[kMaxTiles];  // tiles to read
   u64 red[kWaves];
+  double redd[kWaves];
   u64 out64[4];
   int out32[4];
 };
+
+// Sum over the workgroup in a fixed order, the same in every thread.
+__device__ __forceinline__ double wg_sum(double v, double* sh) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
+  __syncthreads();
+  double t = 0.0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) t += sh[w];
+  return t;
+}
+// Sum over the threads before this one (and of all, in total).
+__device__ __forceinline__ double wg_scan(double v, double* sh, double& total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  double inc = v;
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const double up = __shfl_up(inc, o);
+    if (lane >= o) inc += up;
+  }
+  __syncthreads();
+  if (lane == 63) sh[wave] = inc;
+  __syncthreads();
+  double base = 0.0, t = 0.0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w == wave) base = t;
+    t += sh[w];
+  }
+  total = t;
+  return base + (inc - v);
+}
+__device__ __forceinline__ int wg_min(int v, u64* sh) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = (u64)(uint32_t)v;
+  __syncthreads();
+  v = INT_MAX;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) v = min(v, (int)(uint32_t)sh[w]);
+  return v;
+}
 
 // All threads: sum / exclusive prefix over the workgroup in thread order.
 __device__ __forceinline__ u64 wg_scan(u64 v, u64* sh, u64& total) {
@@ -143,7 +268,7 @@ __device__ __forceinline__ void each4(const SampleK& a, const float* __restrict_
   }
 }
 
-// Sorts list[0..n) ascending, n a power of two.
+// Sorts list[0..n) ascending, n a power of two (two barriers a step, 10 to 78 steps).
 __device__ void bitonic_sort(u64* list, int n) {
   for (int k = 2; k <= n; k <<= 1)
     for (int j = k >> 1; j > 0; j >>= 1) {
@@ -160,18 +285,57 @@ __device__ void bitonic_sort(u64* list, int n) {
   __syncthreads();
 }
 
-// What is kept of a row: tokens above logit tau, those equal to it up to index
-// tau_idx, each with weight >= min_p.
-struct Keep {
-  float tau;
-  int tau_idx;
-};
+// Sorts list[0..n) ascending, keys distinct; list has room for kCap.  Up to kRankMax
+// keys each finds its place by counting the smaller ones (n^2 / 1024 comparisons a
+// thread, three barriers: 0.3 us at 256 keys where the network takes 5), more go
+// through the network, padded to a power of two.
+constexpr int kRankMax = 1024;
+__device__ void sort_list(u64* list, int n) {
+  const int tid = threadIdx.x;
+  int n2 = kWave;
+  while (n2 < n) n2 <<= 1;
+  __syncthreads();
+  for (int i = n + tid; i < n2; i += kThreads) list[i] = ~0ull;
+  if (n > kRankMax) {
+    bitonic_sort(list, n2);
+    return;
+  }
+  int* rank = reinterpret_cast<int*>(list + 2 * kRankMax);
+  rank[tid] = 0;
+  __syncthreads();
+  const int parts = kThreads / n2, i = tid & (n2 - 1), part = tid / n2, per = n2 / parts >= 2 ? n2 / parts : 2;
+  const u64 x = list[i];
+  int cnt = 0;
+  const ulonglong2* pairs = reinterpret_cast<const ulonglong2*>(list);
+  for (int j = part * per; j < min((part + 1) * per, n2); j += 2) {
+    const ulonglong2 y = pairs[j / 2];
+    cnt += (y.x < x) + (y.y < x);
+  }
+  if (parts > 1) {
+    atomicAdd(&rank[i], cnt);
+    __syncthreads();
+    cnt = rank[i];
+  }
+  if (part == 0 && i < n) list[kRankMax + cnt] = x;
+  __syncthreads();
+  if (tid < n) list[tid] = list[kRankMax + tid];
+  __syncthreads();
+}
 
 struct RadixOut {
   uint32_t key;    // of the last token
   uint32_t need;   // how many of the tokens with this key are kept (>= 1)
   u64 mass;        // of the tokens kept
 };
+
+// Bin of d = max - l >= 0: the upper 16 bits of d (8 of exponent, 7 of mantissa)
+// from 2^-8 on; smaller ones share bin 0, from 2^8 on the last.  A bin's relative
+// width is 2^-7, so that it holds a few per cent of a broad row at most, whatever the
+// scale of the logits.
+__device__ __forceinline__ int d_bin(float d) {
+  const int k = (int)(__float_as_uint(d) >> 16) - ((127 - 8) << 7);
+  return min(max(k, 0), kBins - 1);
+}
 
 // Radix search: the last token, in order, at which the count reaches k (by_mass
 // false) or the mass reaches `target`; finite logits only.
@@ -180,7 +344,7 @@ __device__ RadixOut radix_search(const SampleK& a, const float* row, Shared& sh,
   uint32_t prefix = 0, mask = 0;
   u64 before = 0, mass_before = 0;  // of the tokens above the current prefix: count (or mass), mass
   uint32_t ties = 0;
-  u64 tie_w = 0;
+  u64 tie_w = 0, want = target ? target : 1;  // (a target of 0 is met by the very first token: it counts as 1)
   const int shifts[3] = {21, 10, 0}, widths[3] = {11, 11, 10};
   for (int p = 0; p < 3; ++p) {
     const int sft = shifts[p], nb = 1 << widths[p];
@@ -207,13 +371,12 @@ __device__ RadixOut radix_search(const SampleK& a, const float* row, Shared& sh,
     const int b0 = nb - 1 - 2 * (int)threadIdx.x;
     const u64 c0 = b0 >= 0 ? sh.h.count[b0] : 0, c1 = b0 >= 1 ? sh.h.count[b0 - 1] : 0;
     const u64 m0 = b0 >= 0 ? sh.h.mass[b0] : 0, m1 = b0 >= 1 ? sh.h.mass[b0 - 1] : 0;
-    u64 tot;
+    u64 tot, mtot;
     const u64 cb = wg_scan(by_mass ? m0 + m1 : c0 + c1, sh.red, tot);
-    const u64 mb = wg_scan(m0 + m1, sh.red, tot);
+    const u64 mb = wg_scan(m0 + m1, sh.red, mtot);
+    if (p == 0) want = min(want, tot);  // fewer finite logits than top_k
     const u64 s0 = by_mass ? m0 : c0, s1 = by_mass ? m1 : c1;
     const u64 x0 = before + cb, x1 = x0 + s0, x2 = x1 + s1;
-    // (a target of 0 mass is met by the very first token: it counts as 1)
-    const u64 want = target ? target : 1;
     if (x0 < want && want <= x1) {
       sh.out32[0] = b0;
       sh.out64[0] = x0;
@@ -236,7 +399,7 @@ __device__ RadixOut radix_search(const SampleK& a, const float* row, Shared& sh,
     tie_w = sh.out64[2];
   }
   // `ties` equal logits of one weight each
-  const u64 each = tie_w / (ties ? ties : 1), want = target ? target : 1;
+  const u64 each = tie_w / (ties ? ties : 1);
   u64 need = by_mass ? (each ? (want - before + each - 1) / each : 1) : want - before;
   need = need < 1 ? 1 : need > ties ? ties : need;
   return {prefix, (uint32_t)need, mass_before + need * each};
@@ -284,61 +447,290 @@ __device__ int nth_equal(const SampleK& a, const float* row, Shared& sh, float t
   return sh.out32[2];
 }
 
+// The tokens that `in` takes from the tiles whose max is at least `cut`, to sh.list in
+// no order, as sort keys (logit descending, index); returns their number (more than
+// kCap: the list is cut off).
+template <typename F>
+__device__ int collect(const SampleK& a, const float* row, Shared& sh, float cut, F in) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __syncthreads();
+  if (tid < 2) sh.out32[tid] = 0;
+  __syncthreads();
+  for (int t = tid; t < a.ntile; t += kThreads)
+    if (sh.tmax[t] >= cut && sh.tmax[t] > -INFINITY) sh.tiles[atomicAdd(&sh.out32[0], 1)] = (uint16_t)t;
+  __syncthreads();
+  const int nq = sh.out32[0];
+  constexpr int NI = 4;  // tiles in flight per wave
+  for (int i = wave; i < nq; i += NI * kWaves) {
+    f32x4 l[NI];
+    int t[NI];
+#pragma unroll
+    for (int q = 0; q < NI; ++q) {
+      t[q] = sh.tiles[min(i + q * kWaves, nq - 1)];
+      l[q] = tile_quad(a, row, t[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < NI; ++q) {
+      if (i + q * kWaves >= nq) break;  // uniform
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool take = l[q][e] != -INFINITY && in(l[q][e]);
+        const u64 who = __ballot(take);
+        if (!who) continue;
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&sh.out32[1], __popcll(who));
+        at = __builtin_amdgcn_readfirstlane(at) + __popcll(who & ((1ull << lane) - 1));
+        if (take && at < kCap) sh.list[at] = ((u64)~order_key(l[q][e]) << 32) | (uint32_t)(t[q] * kTile + 4 * lane + e);
+      }
+    }
+  }
+  __syncthreads();
+  return sh.out32[1];
+}
+
+// A bound from below of the logits whose bin is at most b (see d_bin).
+__device__ __forceinline__ float bin_floor(float m, int b) {
+  if (b >= kBins - 1) return -INFINITY;
+  const float x = m - __uint_as_float((uint32_t)(b + 1 + ((127 - 8) << 7)) << 16);
+  return x - fabsf(x) * 0x1p-22f;
+}
+
+// The bin in which the running sum over the bins passes `want` (1 <= want <= the
+// sum), from each thread's two bins; `before`: the sum before it.
+__device__ __forceinline__ int find_bin(u64 b0, u64 b1, u64 want, Shared& sh, u64& before) {
+  u64 tot;
+  const u64 x0 = wg_scan(b0 + b1, sh.red, tot), x1 = x0 + b0, x2 = x1 + b1;
+  if (x0 < want && want <= x1) {
+    sh.out32[2] = 2 * threadIdx.x;
+    sh.out64[0] = x0;
+  } else if (x1 < want && want <= x2) {
+    sh.out32[2] = 2 * threadIdx.x + 1;
+    sh.out64[0] = x1;
+  }
+  __syncthreads();
+  before = sh.out64[0];
+  return sh.out32[2];
+}
+
+__device__ __forceinline__ float list_logit(u64 v) { return key_logit(~(uint32_t)(v >> 32)); }
+
 // One workgroup per row.
-__global__ __launch_bounds__(kThreads) void sample_kernel(SampleK a) {
+__global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
   __shared__ Shared sh;
   const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.V;
   const float* row = a.logits + (size_t)r * a.lstride;
-  const float T = a.temperature ? a.temperature[r] : 1.f, P = a.top_p ? a.top_p[r] : 1.f, Q = a.min_p ? a.min_p[r] : 0.f;
-  const float u = a.uniforms[r];
-  int K = a.top_k ? a.top_k[r] : 0;
-  if (K <= 0 || K > V) K = V;
-  const bool greedy = T == 0.f;
-  if (greedy) K = 1;
-
-  // 1. the max; a NaN shows as a count
+  const RowSet s = row_set(a, r);
   float m = -INFINITY;
-  int nan = 0;
-  each4(a, row, [&](int, int, const float(&l)[4]) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      m = fmaxf(m, l[e]);
-      nan |= l[e] != l[e];
-    }
-  });
-  for (int o = 32; o > 0; o >>= 1) {
-    m = fmaxf(m, __shfl_xor(m, o));
-    nan |= __shfl_xor(nan, o);
+  for (int t = tid; t < a.ntile; t += kThreads) {
+    sh.tmax[t] = a.tmax[(size_t)r * a.ntile + t];
+    m = fmaxf(m, sh.tmax[t]);
+    if (s.mass) sh.tmass[t] = a.tmass[(size_t)r * a.ntile + t];
   }
-  if (lane == 0) sh.red[wave] = ((u64)(nan != 0) << 32) | __float_as_uint(m);
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  if (lane == 0) sh.red[wave] = __float_as_uint(m);
   __syncthreads();
-  m = -INFINITY;
-  for (int w = 0; w < kWaves; ++w) {
-    m = fmaxf(m, __uint_as_float((uint32_t)sh.red[w]));
-    nan |= (int)(sh.red[w] >> 32);
-  }
-  const bool ok = T >= 0.f && T < INFINITY && P >= 0.f && Q >= 0.f && Q <= 1.f && u >= 0.f && u < 1.f && !nan &&
-                  m > -INFINITY && m < INFINITY;
-  if (!ok) {
+  for (int w = 0; w < kWaves; ++w) m = fmaxf(m, __uint_as_float((uint32_t)sh.red[w]));
+  if (!s.ok || !(m > -INFINITY && m < INFINITY)) {  // (a NaN shows as +inf)
     if (tid == 0) {
       a.tokens[r] = -1;
+      a.head[r] = {0.0, m, INFINITY, -1};
       flag_error(a.err, kErrSampling);
     }
-    if (a.probs)
-      for (int j = tid; j < V; j += kThreads) a.probs[(size_t)r * a.pstride + j] = 0.f;
     return;
   }
-  const double md = m, scale = 1.4426950408889634074 / (greedy ? 1.0 : (double)T), mind = Q;
-  auto weight64 = [&](float l) { return exp2_64(((double)l - md) * scale); };
-  auto weight = [&](float l) { return fixed44(weight64(l)); };
-  const bool by_count = K < V, by_mass = P < 1.f;
+  const double md = m, mind = s.Q;
+  auto weight = [&](float l) { return exp2_64(((double)l - md) * s.scale); };
+  auto done = [&](int token, float tau, int tau_idx, double total) {
+    if (tid == 0) {
+      a.tokens[r] = token;
+      a.head[r] = {1.0 / total, m, tau, tau_idx};
+    }
+  };
 
-  Keep keep{-INFINITY, V};
-  u64 total = 0;
-  int token = -1;
+  if (s.greedy) {  // the first tile that holds the max, and its first place there
+    int first = INT_MAX;
+    for (int t = tid; t < a.ntile; t += kThreads)
+      if (sh.tmax[t] == m) {
+        first = t;
+        break;
+      }
+    first = wg_min(first, sh.red);
+    int at = INT_MAX;
+    if (wave == 0) {
+      const f32x4 l = tile_quad(a, row, first);
+#pragma unroll
+      for (int e = 3; e >= 0; --e)
+        if (l[e] == m) at = first * kTile + 4 * lane + e;
+    }
+    at = wg_min(at, sh.red);
+    done(at, m, at, 1.0);
+    return;
+  }
+
+  double mass = 0.0;  // of the whole row
+  if (s.mass) {
+    for (int t = tid; t < a.ntile; t += kThreads) {
+      sh.tmass[t] = sh.tmax[t] > -INFINITY ? sh.tmass[t] * weight(sh.tmax[t]) : 0.0;
+      mass += sh.tmass[t];
+    }
+    mass = wg_sum(mass, sh.redd);
+  }
+
+  if (!s.by_count && !s.by_mass && s.Q == 0.f) {
+    // no truncation: the tile in which the running sum passes u * total, then the token
+    const double m0 = 2 * tid < a.ntile ? sh.tmass[2 * tid] : 0.0, m1 = 2 * tid + 1 < a.ntile ? sh.tmass[2 * tid + 1] : 0.0;
+    double total;
+    const double base = wg_scan(m0 + m1, sh.redd, total);
+    const double t = (double)s.u * total;
+    int tile = base + m0 > t && m0 > 0.0 ? 2 * tid : base + (m0 + m1) > t && m1 > 0.0 ? 2 * tid + 1 : INT_MAX;
+    tile = wg_min(tile, sh.red);
+    if (tile == INT_MAX) {  // rounding: the last tile with any weight
+      int last = m1 > 0.0 ? 2 * tid + 1 : m0 > 0.0 ? 2 * tid : -1;
+      tile = -wg_min(-last, sh.red);
+    }
+    if (tid == tile / 2) sh.redd[0] = base + (tile & 1 ? m0 : 0.0);
+    __syncthreads();
+    const double before = sh.redd[0];
+    if (wave == 0) {
+      const f32x4 l = tile_quad(a, row, tile);
+      double w[4], ls = 0.0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        w[e] = weight(l[e]);
+        ls += w[e];
+      }
+      double inc = ls;
+      for (int o = 1; o < kWave; o <<= 1) {
+        const double up = __shfl_up(inc, o);
+        if (lane >= o) inc += up;
+      }
+      double run = before + (inc - ls);
+      int at = INT_MAX, last = -1;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        run += w[e];
+        const int j = tile * kTile + 4 * lane + e;
+        if (w[e] > 0.0) {
+          if (run > t && at == INT_MAX) at = j;
+          last = j;
+        }
+      }
+      for (int o = 32; o > 0; o >>= 1) {
+        at = min(at, __shfl_xor(at, o));
+        last = max(last, __shfl_xor(last, o));
+      }
+      if (lane == 0) sh.out32[3] = at == INT_MAX ? last : at;
+    }
+    __syncthreads();
+    done(sh.out32[3], -INFINITY, V, total);
+    return;
+  }
+
+  // A logit that every kept token reaches.  top-k: the bin of the K-th largest tile
+  // max (each tile has a token that large); with fewer tiles than K, some tile's, the
+  // smallest at last.  top-p alone: guesses, lowered while the tokens above fall short
+  // of the target.  min-p alone: its own border (a little below: the test itself decides).
+  float cut = -INFINITY;
+  u64 b0 = 0, b1 = 0;  // this thread's two bins of the tile maxima
+  if (s.by_count) {
+    __syncthreads();
+    for (int i = tid; i < kBins; i += kThreads) sh.h.count[i] = 0;
+    __syncthreads();
+    for (int t = tid; t < a.ntile; t += kThreads) atomicAdd(&sh.h.count[sh.tmax[t] > -INFINITY ? d_bin(m - sh.tmax[t]) : kBins - 1], 1u);
+    __syncthreads();
+    b0 = sh.h.count[2 * tid];
+    b1 = sh.h.count[2 * tid + 1];
+  }
+  constexpr int kGuesses = 5;
+  constexpr float kGuess[kGuesses] = {-5.f, -8.f, -12.f, -16.f, -24.f};  // log2 of the weight
+  int n = 0;
   bool listed = false;
-  if (by_count || by_mass) {
-    // 2. the histogram
+  double target = 0.0;
+  for (int round = 0; !listed; ++round) {
+    if (s.by_count) {
+      // ranks of the tile maxima: K, or with fewer tiles 1/2, 3/4 and all of them
+      const int rank = s.K <= a.ntile ? s.K : round == 0 ? (a.ntile + 1) / 2 : round == 1 ? (3 * a.ntile + 3) / 4 : a.ntile;
+      u64 before;
+      cut = bin_floor(m, find_bin(b0, b1, (u64)rank, sh, before));
+    } else {
+      cut = !s.by_mass ? (float)(md + (log2(mind) - 1e-6) / s.scale) : round < kGuesses ? (float)(md + kGuess[round] / s.scale) : -INFINITY;
+      cut = fminf(cut, m) - fabsf(cut) * 0x1p-22f;
+    }
+    n = collect(a, row, sh, cut, [&](float l) { return l >= cut; });
+    if (n > kCap) break;
+    if (s.by_count) {
+      if (n < s.K && cut > -INFINITY) {
+        if (s.K <= a.ntile || round >= 2) break;  // (more than one token per tile is kept)
+        continue;
+      }
+    } else if (s.by_mass) {
+      double w = 0.0;
+      for (int i = tid; i < n; i += kThreads) w += weight(list_logit(sh.list[i]));
+      w = wg_sum(w, sh.redd);
+      target = (double)s.P * mass;
+      if (w < target && cut > -INFINITY) continue;
+    }
+    sort_list(sh.list, n);
+    listed = true;
+  }
+  if (listed) {
+    const int kk = min(s.K, n);
+    // prefix sums of the weights, four tokens a thread
+    double w[4], ls = 0.0, tot;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = 4 * tid + e;
+      w[e] = i < kk ? weight(list_logit(sh.list[i])) : 0.0;
+      ls += w[e];
+    }
+    double run = wg_scan(ls, sh.redd, tot);
+    if (!s.by_mass) target = INFINITY;
+    else if (s.by_count) target = (double)s.P * tot;
+    // kept: i < kk, the sum before it below the target (or i = 0), w >= min_p
+    int cnt = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = 4 * tid + e;
+      cnt += i < kk && (i == 0 || run < target) && w[e] >= mind;
+      run += w[e];
+    }
+    u64 all;
+    wg_scan((u64)cnt, sh.red, all);
+    const int L = (int)all;
+    const u64 last = sh.list[L - 1];
+    // the kept tokens in index order
+    __syncthreads();
+    for (int i = tid; i < L; i += kThreads) sh.list[i] = (sh.list[i] << 32) | (sh.list[i] >> 32);
+    sort_list(sh.list, L);
+    ls = 0.0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = 4 * tid + e;
+      w[e] = i < L ? weight(key_logit(~(uint32_t)sh.list[i])) : 0.0;
+      ls += w[e];
+    }
+    double total;
+    run = wg_scan(ls, sh.redd, total);
+    const double t = (double)s.u * total;
+    int at = INT_MAX;  // the first whose running sum passes t; the last if rounding leaves none
+#pragma unroll
+    for (int e = 3; e >= 0; --e) {
+      double incl = run;
+      for (int f = 0; f <= e; ++f) incl += w[f];
+      if (4 * tid + e < L && incl > t) at = 4 * tid + e;
+    }
+    at = min(wg_min(at, sh.red), L - 1);
+    done((int)(uint32_t)(sh.list[at] >> 32), list_logit(last), (int)(uint32_t)last, total);
+    return;
+  }
+
+  // The long way: a histogram of the whole row over d_bin finds the bin of the last
+  // token, a list of that bin's tokens the token; a bin that holds more than the list
+  // (equal logits by the thousand) is searched by the logits' bits.
+  auto weight44 = [&](float l) { return fixed44(weight(l)); };
+  float tau = -INFINITY;
+  int tau_idx = V;
+  if (s.by_count || s.by_mass) {
     __syncthreads();
     for (int i = tid; i < kBins; i += kThreads) {
       sh.h.mass[i] = 0;
@@ -350,186 +742,159 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleK a) {
       for (int e = 0; e < 4; ++e)
         if (l[e] != -INFINITY) {
           const int bin = d_bin(m - l[e]);
-          atomicAdd(&sh.h.count[bin], 1u);
-          if (!by_count) {
-            const u64 w = weight(l[e]);
+          if (s.by_count) atomicAdd(&sh.h.count[bin], 1u);
+          if (s.by_mass) {
+            const u64 w = weight44(l[e]);
             if (w) atomicAdd(&sh.h.mass[bin], w);
           }
         }
     });
     __syncthreads();
+    const u64 c0 = sh.h.count[2 * tid], c1 = sh.h.count[2 * tid + 1], m0 = sh.h.mass[2 * tid], m1 = sh.h.mass[2 * tid + 1];
     u64 ctot, mtot;
-    const u64 c0 = sh.h.count[2 * tid], c1 = sh.h.count[2 * tid + 1];
-    const u64 m0 = by_count ? 0 : sh.h.mass[2 * tid], m1 = by_count ? 0 : sh.h.mass[2 * tid + 1];
-    const u64 cb = wg_scan(c0 + c1, sh.red, ctot), mb = wg_scan(m0 + m1, sh.red, mtot);
-    // the bin where the count reaches min(K, finite tokens), or the mass the target
-    const u64 kk = min((u64)K, ctot);
-    u64 target = by_count ? 0 : (u64)ceil((double)P * (double)mtot);
-    {
-      const u64 want = by_count ? kk : (target ? target : 1);
-      const u64 x0 = by_count ? cb : mb, s0 = by_count ? c0 : m0, s1 = by_count ? c1 : m1;
-      if (x0 < want && want <= x0 + s0) {
-        sh.out32[0] = 2 * tid;
-        sh.out64[0] = cb + c0;
-      } else if (x0 + s0 < want && want <= x0 + s0 + s1) {
-        sh.out32[0] = 2 * tid + 1;
-        sh.out64[0] = cb + c0 + c1;
+    wg_scan(c0 + c1, sh.red, ctot);
+    wg_scan(m0 + m1, sh.red, mtot);
+    // the last token at which the count (or the mass) reaches `want`, and the mass up to it
+    auto search = [&](bool by_mass, u64 want) {
+      u64 before, mbefore = 0;
+      const int bin = by_mass ? find_bin(m0, m1, want, sh, before) : find_bin(c0, c1, want, sh, before);
+      if (by_mass) {
+        mbefore = before;
+      } else if (s.by_mass) {  // the mass before that bin
+        wg_scan((2 * tid < bin ? m0 : 0) + (2 * tid + 1 < bin ? m1 : 0), sh.red, mbefore);
       }
-    }
-    __syncthreads();
-    const int bin = sh.out32[0];
-    const int n = (int)min(sh.out64[0], (u64)kCap + 1);
-    if (n <= kCap) {
-      // 3. the tokens up to that bin, sorted by (logit descending, index)
-      listed = true;
-      if (tid == 0) sh.out32[1] = 0;
-      __syncthreads();
-      each4(a, row, [&](int, int j, const float(&l)[4]) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (l[e] != -INFINITY && d_bin(m - l[e]) <= bin) {
-            const int at = atomicAdd(&sh.out32[1], 1);
-            if (at < kCap) sh.list[at] = ((u64)~order_key(l[e]) << 32) | (uint32_t)(j + e);
-          }
-      });
-      __syncthreads();
-      int n2 = 2;
-      while (n2 < n) n2 <<= 1;
-      for (int i = n + tid; i < n2; i += kThreads) sh.list[i] = ~0ull;
-      bitonic_sort(sh.list, n2);
-      // prefix sums of the weights, four tokens a thread
-      u64 w[4], ls = 0, tot;
-      double wd[4];
+      const int nb = collect(a, row, sh, bin_floor(m, bin), [&](float l) { return d_bin(m - l) == bin; });
+      if (nb > kCap) {
+        const RadixOut x = radix_search(a, row, sh, by_mass, want, weight44);
+        tau = key_logit(x.key);
+        tau_idx = nth_equal(a, row, sh, tau, x.need);
+        return x.mass;
+      }
+      sort_list(sh.list, nb);
+      u64 w[4], ls = 0, all;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int i = 4 * tid + e;
-        wd[e] = i < n && i < (int)kk ? weight64(key_logit(~(uint32_t)(sh.list[i] >> 32))) : 0.0;
-        w[e] = fixed44(wd[e]);
+        w[e] = i < nb && (by_mass || s.by_mass) ? weight44(list_logit(sh.list[i])) : 0;
         ls += w[e];
       }
-      u64 run = wg_scan(ls, sh.red, tot);
-      if (by_count) target = by_mass ? (u64)ceil((double)P * (double)tot) : ~0ull;
-      // kept: i < kk, the sum before it below the target (or i = 0), w >= min_p
-      int cnt = 0;
+      u64 run = mbefore + wg_scan(ls, sh.red, all);
+      int at = INT_MAX;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int i = 4 * tid + e;
-        cnt += i < n && i < (int)kk && (i == 0 || run < target) && wd[e] >= mind;
+        const bool hit = i < nb && (by_mass ? run < want && want <= run + w[e] : before + (u64)i + 1 == want);
         run += w[e];
+        if (hit) {
+          at = i;
+          sh.out64[1] = run;
+        }
       }
-      u64 all;
-      wg_scan((u64)cnt, sh.red, all);
-      const int L = (int)all;
-      const u64 last = sh.list[L - 1];
-      keep = {key_logit(~(uint32_t)(last >> 32)), (int)(uint32_t)last};
-      // the kept tokens in index order
-      int l2 = 2;
-      while (l2 < L) l2 <<= 1;
-      __syncthreads();
-      for (int i = tid; i < l2; i += kThreads) {
-        const u64 v = i < L ? sh.list[i] : ~0ull;
-        sh.list[i] = (v << 32) | (v >> 32);
-      }
-      bitonic_sort(sh.list, l2);
-      ls = 0;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int i = 4 * tid + e;
-        w[e] = i < L ? weight(key_logit(~(uint32_t)sh.list[i])) : 0;
-        ls += w[e];
-      }
-      run = wg_scan(ls, sh.red, total);
-      const u64 t = (u64)((double)u * (double)total);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (run <= t && t < run + w[e]) sh.out32[2] = (int)(uint32_t)(sh.list[4 * tid + e] >> 32);
-        run += w[e];
-      }
-      __syncthreads();
-      token = sh.out32[2];
-    } else {
-      RadixOut x{};
-      if (by_count) {
-        x = radix_search(a, row, sh, false, kk, weight);
-        target = (u64)ceil((double)P * (double)x.mass);
-      }
-      if (by_mass) x = radix_search(a, row, sh, true, target, weight);
-      const float tau = key_logit(x.key);
-      keep = {tau, nth_equal(a, row, sh, tau, x.need)};
+      at = min(wg_min(at, sh.red), nb - 1);
+      tau = list_logit(sh.list[at]);
+      tau_idx = (int)(uint32_t)sh.list[at];
+      return sh.out64[1];
+    };
+    u64 have = mtot;
+    if (s.by_count) have = search(false, min((u64)s.K, ctot));
+    // (by mass alone: of the tiles' sums, as on the short way)
+    if (s.by_mass) {
+      const double of = s.by_count ? (double)have : mass * 0x1p44;
+      search(true, min(max((u64)ceil((double)s.P * of), (u64)1), mtot));
     }
   }
-  auto kept = [&](float l, int j) { return l != -INFINITY && (l > keep.tau || (l == keep.tau && j <= keep.tau_idx)); };
-  if (!listed) {
-    // the draw over the whole row: weights of 256-token tiles, the tile, the token
-    __syncthreads();
-    for (int i = tid; i < kMaxTiles; i += kThreads) sh.tsum[i] = 0;
-    __syncthreads();
-    each4(a, row, [&](int rd, int j, const float(&l)[4]) {
-      u64 s = 0;
+  auto kept = [&](float l, int j) { return l != -INFINITY && (l > tau || (l == tau && j <= tau_idx)); };
+  // weights of 256-token tiles, the tile, the token
+  __syncthreads();
+  for (int i = tid; i < kMaxTiles; i += kThreads) sh.tsum[i] = 0;
+  __syncthreads();
+  each4(a, row, [&](int rd, int j, const float(&l)[4]) {
+    u64 sum = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (kept(l[e], j + e)) {
+        const double w = weight(l[e]);
+        if (w >= mind) sum += fixed44(w);
+      }
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+    if (lane == 0) sh.tsum[rd * kWaves + wave] = sum;
+  });
+  __syncthreads();
+  const u64 s0 = sh.tsum[2 * tid], s1 = sh.tsum[2 * tid + 1];
+  u64 total;
+  const u64 base = wg_scan(s0 + s1, sh.red, total);
+  const u64 t = (u64)((double)s.u * (double)total);
+  if (base <= t && t < base + s0 + s1) {
+    const bool second = t >= base + s0;
+    sh.out32[0] = 2 * tid + second;
+    sh.out64[0] = base + (second ? s0 : 0);
+  }
+  __syncthreads();
+  if (wave == 0) {
+    const int j = sh.out32[0] * kTile + 4 * lane;
+    u64 w[4], ls = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      w[e] = 0;
+      if (j + e < V && kept(row[j + e], j + e)) {
+        const double x = weight(row[j + e]);
+        if (x >= mind) w[e] = fixed44(x);
+      }
+      ls += w[e];
+    }
+    u64 inc = ls;
+    for (int o = 1; o < kWave; o <<= 1) {
+      const u64 up = __shfl_up(inc, o);
+      if (lane >= o) inc += up;
+    }
+    u64 run = sh.out64[0] + inc - ls;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (run <= t && t < run + w[e]) sh.out32[2] = j + e;
+      run += w[e];
+    }
+  }
+  __syncthreads();
+  done(sh.out32[2], tau, tau_idx, (double)total * 0x1p-44);
+}
+
+// The distribution.  grid (rows, ceil(ntile / kTilesPerWg)).
+__global__ __launch_bounds__(256) void sample_probs_kernel(SampleK a) {
+  const int r = blockIdx.x, lane = threadIdx.x & 63, t0 = blockIdx.y * kTilesPerWg + (threadIdx.x >> 6) * kWaveTiles;
+  const float* row = a.logits + (size_t)r * a.lstride;
+  float* out = a.probs + (size_t)r * a.pstride;
+  const RowHead h = a.head[r];
+  const RowSet s = row_set(a, r);
+  f32x4 l[kWaveTiles];
+  bool any[kWaveTiles];
+#pragma unroll
+  for (int i = 0; i < kWaveTiles; ++i) {
+    any[i] = false;
+    if (t0 + i < a.ntile) {
+      const float m = a.tmax[(size_t)r * a.ntile + t0 + i];
+      any[i] = h.inv > 0.0 && m >= h.tau && m > -INFINITY;
+      if (any[i]) l[i] = tile_quad(a, row, t0 + i);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kWaveTiles; ++i) {
+    if (t0 + i >= a.ntile) break;
+    const int j = (t0 + i) * kTile + 4 * lane;
+    f32x4 p = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (any[i]) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool kept = l[i][e] != -INFINITY && (l[i][e] > h.tau || (l[i][e] == h.tau && j + e <= h.tau_idx));
+        const double w = kept ? exp2_64(((double)l[i][e] - (double)h.max) * s.scale) : 0.0;
+        p[e] = w >= (double)s.Q ? (float)(w * h.inv) : 0.f;
+      }
+    }
+    if (a.pvec && j + 3 < a.V)
+      *reinterpret_cast<f32x4*>(out + j) = p;
+    else
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (kept(l[e], j + e)) {
-          const double w = weight64(l[e]);
-          if (w >= mind) s += fixed44(w);
-        }
-      for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
-      if (lane == 0) sh.tsum[rd * kWaves + wave] = s;
-    });
-    __syncthreads();
-    const u64 s0 = sh.tsum[2 * tid], s1 = sh.tsum[2 * tid + 1];
-    const u64 base = wg_scan(s0 + s1, sh.red, total);
-    const u64 t = (u64)((double)u * (double)total);
-    if (base <= t && t < base + s0 + s1) {
-      const bool second = t >= base + s0;
-      sh.out32[0] = 2 * tid + second;
-      sh.out64[0] = base + (second ? s0 : 0);
-    }
-    __syncthreads();
-    if (wave == 0) {
-      const int j = sh.out32[0] * kTile + 4 * lane;
-      u64 w[4], ls = 0;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        w[e] = 0;
-        if (j + e < V && kept(row[j + e], j + e)) {
-          const double x = weight64(row[j + e]);
-          if (x >= mind) w[e] = fixed44(x);
-        }
-        ls += w[e];
-      }
-      u64 inc = ls;
-      for (int o = 1; o < kWave; o <<= 1) {
-        const u64 up = __shfl_up(inc, o);
-        if (lane >= o) inc += up;
-      }
-      u64 run = sh.out64[0] + inc - ls;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (run <= t && t < run + w[e]) sh.out32[2] = j + e;
-        run += w[e];
-      }
-    }
-    __syncthreads();
-    token = sh.out32[2];
-  }
-  if (tid == 0) a.tokens[r] = token;
-  if (a.probs) {
-    const double inv = 0x1p44 / (double)total;
-    float* out = a.probs + (size_t)r * a.pstride;
-    each4(a, row, [&](int, int j, const float(&l)[4]) {
-      f32x4 p;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const double w = kept(l[e], j + e) ? weight64(l[e]) : 0.0;
-        p[e] = w >= mind ? (float)(w * inv) : 0.f;
-      }
-      if (a.pvec && j + 3 < V)
-        *reinterpret_cast<f32x4*>(out + j) = p;
-      else
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (j + e < V) out[j + e] = p[e];
-    });
+        if (j + e < a.V) out[j + e] = p[e];
   }
 }
 
@@ -545,11 +910,28 @@ bool sample_sizes(int32_t rows, int32_t vocab) {
     return !set_last_error(NJ_EINVAL, "sample: rows must be >= 1 and vocab in 1 .. %d", kSampleMaxVocab);
   return true;
 }
+
+// [error word][row heads][tile sums][tile maxima]
+struct SampleLayout {
+  size_t head, mass, max, total;
+};
+SampleLayout sample_layout(int32_t rows, int32_t vocab) {
+  auto al = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  const size_t tiles = (size_t)rows * ((vocab + kTile - 1) / kTile);
+  SampleLayout L{};
+  L.head = 256;
+  L.mass = L.head + al((size_t)rows * sizeof(RowHead));
+  L.max = L.mass + al(tiles * 8);
+  L.total = L.max + al(tiles * 4);
+  return L;
+}
 }  // namespace
 
 extern "C" {
 
-size_t nightjar_sample_workspace_bytes(int32_t rows, int32_t vocab) { return sample_sizes(rows, vocab) ? 256 : 0; }
+size_t nightjar_sample_workspace_bytes(int32_t rows, int32_t vocab) {
+  return sample_sizes(rows, vocab) ? sample_layout(rows, vocab).total : 0;
+}
 
 int nightjar_sample(const float* logits, int64_t logits_stride, int32_t rows, int32_t vocab, const float* temperature,
                     const int32_t* top_k, const float* top_p, const float* min_p, const float* uniforms,
@@ -569,10 +951,24 @@ int nightjar_sample(const float* logits, int64_t logits_stride, int32_t rows, in
   if (((uintptr_t)workspace & 255) != 0) return set_last_error(NJ_EINVAL, "sample: workspace must be 256-byte aligned");
   const bool lv = ((uintptr_t)logits & 15) == 0 && logits_stride % 4 == 0;
   const bool pv = ((uintptr_t)probs & 15) == 0 && probs_stride % 4 == 0;
-  SampleK a{logits, logits_stride, vocab, temperature, top_k, top_p, min_p, uniforms, tokens, probs, probs_stride,
-            static_cast<int*>(workspace), lv, pv};
-  hipLaunchKernelGGL(sample_kernel, dim3(rows), dim3(kThreads), 0, (hipStream_t)stream, a);
-  const hipError_t e = hipGetLastError();
+  const SampleLayout L = sample_layout(rows, vocab);
+  char* ws = static_cast<char*>(workspace);
+  const int ntile = (vocab + kTile - 1) / kTile;
+  SampleK a{logits, logits_stride, vocab, ntile, temperature, top_k, top_p, min_p, uniforms, tokens, probs, probs_stride,
+            reinterpret_cast<int*>(ws), reinterpret_cast<double*>(ws + L.mass), reinterpret_cast<float*>(ws + L.max),
+            reinterpret_cast<RowHead*>(ws + L.head), lv, pv};
+  hipStream_t s = (hipStream_t)stream;
+  const dim3 grid(rows, (ntile + kTilesPerWg - 1) / kTilesPerWg);
+  hipLaunchKernelGGL(sample_tiles_kernel, grid, dim3(256), 0, s, a);
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess) {
+    hipLaunchKernelGGL(sample_rows_kernel, dim3(rows), dim3(kThreads), 0, s, a);
+    e = hipGetLastError();
+  }
+  if (e == hipSuccess && probs) {
+    hipLaunchKernelGGL(sample_probs_kernel, grid, dim3(256), 0, s, a);
+    e = hipGetLastError();
+  }
   return e == hipSuccess ? NJ_OK : set_last_error(NJ_EHIP, "sample: %s", hipGetErrorString(e));
 }
 

@@ -162,3 +162,26 @@ def test_graph_replay():
         torch.cuda.synchronize()
         assert torch.equal(tok, want[0]) and torch.equal(probs, want[1])
     assert device_error(ws) == 0
+
+
+@pytest.mark.parametrize("kw", [dict(k=10000), dict(k=10000, p=0.9), dict(k=4500), dict(p=0.99), dict(k=20), dict(p=0.3)])
+def test_few_tokens_left_of_a_large_vocabulary(kw):
+    """A mask that leaves 5000 tokens in a few places: fewer than top_k, more than a sorted list holds."""
+    rng = np.random.default_rng(12)
+    V = 128256
+    l = np.full((2, V), -np.inf, np.float32)
+    l[0, 70000:75000] = 0.3 * rng.standard_normal(5000)
+    l[1, rng.permutation(V)[:5000]] = 0.3 * rng.standard_normal(5000)
+    _check(l, rng.random(2).astype(np.float32), **kw)
+
+
+def test_same_result_whatever_the_batch():
+    """A row gives the same token and the same bits alone and among others."""
+    rng = np.random.default_rng(13)
+    l = (2 * rng.standard_normal((9, 50000))).astype(np.float32)
+    u = rng.random(9).astype(np.float32)
+    for kw in (dict(), dict(p=0.9), dict(k=30), dict(k=6000, p=0.9)):
+        tok, probs, _ = _run(l, u, **kw)
+        for r in (0, 4, 8):
+            t1, p1, _ = _run(l[r:r + 1], u[r:r + 1], **kw)
+            assert t1[0] == tok[r] and np.array_equal(p1[0], probs[r])
