@@ -34,29 +34,28 @@ namespace {
 constexpr int kErrSampling = 32;  // NJ_DEV_BAD_SAMPLING
 constexpr int kThreads = 1024, kWaves = kThreads / kWave;
 constexpr int kBins = 2048;
-constexpr int kCap = 4096;        // tokens of the sorted list
+constexpr int kShort = 1024;      // tokens that the short way sorts, one a thread
+constexpr int kCap = 4096;        // tokens that the long way lists
 constexpr int kTile = 256;        // tokens per running-sum tile (four per lane of a wave)
 constexpr int kMaxTiles = 2048;   // V <= 524288
 typedef unsigned long long u64;
 
-// exp2(x) for x <= 0 in 64 bits: 2^n times the Taylor series of 2^f, |f| <= 1/2
-// (the terms behind f^11 are below 1e-14).  exp2(0) = 1 exactly; below 2^-200: 0.
+// exp2(x) for x <= 0 in 64 bits: 2^n (1 + f q(f)), |f| <= 1/2, where q is the polynomial
+// that meets (2^f - 1) / f at the nine Chebyshev points of that interval: relative error
+// below 4e-14.  exp2(0) = 1 exactly, exp2(-inf) = 0.
 __device__ __forceinline__ double exp2_64(double x) {
-  if (!(x > -200.0)) return 0.0;
-  const double n = rint(x), f = (x - n) * 0.69314718055994530942;
-  double p = 1.0 / 39916800.0;
-  p = fma(p, f, 1.0 / 3628800.0);
-  p = fma(p, f, 1.0 / 362880.0);
-  p = fma(p, f, 1.0 / 40320.0);
-  p = fma(p, f, 1.0 / 5040.0);
-  p = fma(p, f, 1.0 / 720.0);
-  p = fma(p, f, 1.0 / 120.0);
-  p = fma(p, f, 1.0 / 24.0);
-  p = fma(p, f, 1.0 / 6.0);
-  p = fma(p, f, 0.5);
-  p = fma(p, f, 1.0);
-  p = fma(p, f, 1.0);
-  return p * __longlong_as_double((long long)(1023 + (int)n) << 52);
+  x = fmax(x, -2000.0);
+  const double n = rint(x), f = x - n;
+  double p = 0x1.b63871ee00eb4p-24;
+  p = fma(p, f, 0x1.63d13637e6140p-20);
+  p = fma(p, f, 0x1.ffcb952643063p-17);
+  p = fma(p, f, 0x1.4308ac85a8ca4p-13);
+  p = fma(p, f, 0x1.5d87fe86f8453p-10);
+  p = fma(p, f, 0x1.3b2ab7181b769p-7);
+  p = fma(p, f, 0x1.c6b08d7047e8ap-5);
+  p = fma(p, f, 0x1.ebfbdff823cedp-3);
+  p = fma(p, f, 0x1.62e42fefa39efp-1);
+  return ldexp(fma(p, f, 1.0), (int)n);
 }
 __device__ __forceinline__ u64 fixed44(double w) { return (u64)(w * 0x1p44 + 0.5); }
 
@@ -129,6 +128,56 @@ __device__ __forceinline__ f32x4 tile_quad(const SampleK& a, const float* __rest
   return l;
 }
 
+// Running sums over a wave (inclusive) in a fixed order, each step one move between
+// lanes in registers; lane 63 ends with the wave's.
+template <int CTRL, int ROWS, typename T>
+__device__ __forceinline__ T dpp_add(T v) {
+  union {
+    T v;
+    int h[sizeof(T) / 4];
+  } x{v}, y;
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(T) / 4); ++i) y.h[i] = __builtin_amdgcn_update_dpp(0, x.h[i], CTRL, ROWS, 0xf, false);
+  return v + y.v;
+}
+template <typename T>
+__device__ __forceinline__ T row_scan(T v) {  // over each 16 lanes
+  v = dpp_add<0x111, 0xf>(v);  // row_shr 1, 2, 4, 8
+  v = dpp_add<0x112, 0xf>(v);
+  v = dpp_add<0x114, 0xf>(v);
+  return dpp_add<0x118, 0xf>(v);
+}
+template <typename T>
+__device__ __forceinline__ T wave_scan(T v) {
+  v = row_scan(v);
+  v = dpp_add<0x142, 0xa>(v);     // row_bcast 15, 31
+  return dpp_add<0x143, 0xc>(v);
+}
+template <typename T>
+__device__ __forceinline__ T lane_value(T v, int lane) {
+  union {
+    T v;
+    int h[sizeof(T) / 4];
+  } x{v};
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(T) / 4); ++i) x.h[i] = __builtin_amdgcn_readlane(x.h[i], lane);
+  return x.v;
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp_max(float v) {
+  const int i = __float_as_int(v);
+  return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(i, i, CTRL, ROWS, 0xf, false)));
+}
+__device__ __forceinline__ float wave_max(float v) {
+  v = dpp_max<0x111, 0xf>(v);
+  v = dpp_max<0x112, 0xf>(v);
+  v = dpp_max<0x114, 0xf>(v);
+  v = dpp_max<0x118, 0xf>(v);
+  v = dpp_max<0x142, 0xa>(v);
+  v = dpp_max<0x143, 0xc>(v);
+  return lane_value(v, 63);
+}
+
 // grid (rows, ceil(ntile / kTilesPerWg)); a wave reads its four tiles at once.
 constexpr int kWaveTiles = 4, kTilesPerWg = 4 * kWaveTiles;
 __global__ __launch_bounds__(256) void sample_tiles_kernel(SampleK a) {
@@ -144,19 +193,16 @@ __global__ __launch_bounds__(256) void sample_tiles_kernel(SampleK a) {
     if (t0 + i >= a.ntile) break;  // uniform
     float m = fmaxf(fmaxf(l[i][0], l[i][1]), fmaxf(l[i][2], l[i][3]));
     const bool nan = l[i][0] != l[i][0] || l[i][1] != l[i][1] || l[i][2] != l[i][2] || l[i][3] != l[i][3];
-    if (nan) m = INFINITY;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    m = wave_max(nan ? INFINITY : m);
     if (lane == 0) a.tmax[(size_t)r * a.ntile + t0 + i] = m;
     if (s.mass) {
       double w = 0.0;
       if (m > -INFINITY && m < INFINITY) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) w += exp2_64(((double)l[i][e] - (double)m) * s.scale);
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) w += __shfl_xor(w, o);
+        w = wave_scan(w);
       }
-      if (lane == 0) a.tmass[(size_t)r * a.ntile + t0 + i] = w;
+      if (lane == 63) a.tmass[(size_t)r * a.ntile + t0 + i] = w;
     }
   }
 }
@@ -176,100 +222,69 @@ struct Shared {
   __attribute__((aligned(16))) float tmax[kMaxTiles];
   uint16_t tiles[kMaxTiles];  // tiles to read
   u64 red[kWaves];
-  double redd[kWaves];
   u64 out64[4];
   int out32[4];
 };
 
-// Sum over the workgroup in a fixed order, the same in every thread.
-__device__ __forceinline__ double wg_sum(double v, double* sh) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
-  __syncthreads();
-  double t = 0.0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) t += sh[w];
-  return t;
-}
-// Sum over the threads before this one (and of all, in total).
-__device__ __forceinline__ double wg_scan(double v, double* sh, double& total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  double inc = v;
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const double up = __shfl_up(inc, o);
-    if (lane >= o) inc += up;
-  }
+// Sum over the threads before this one (and of all, in total), in a fixed order.
+template <typename T>
+__device__ __forceinline__ T wg_scan(T v, void* scratch, T& total) {
+  T* sh = static_cast<T*>(scratch);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const T inc = wave_scan(v);
   __syncthreads();
   if (lane == 63) sh[wave] = inc;
   __syncthreads();
-  double base = 0.0, t = 0.0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w == wave) base = t;
-    t += sh[w];
-  }
-  total = t;
-  return base + (inc - v);
+  const T x = row_scan(sh[lane & (kWaves - 1)]);
+  total = lane_value(x, kWaves - 1);
+  return (wave ? lane_value(x, wave - 1) : T(0)) + (inc - v);
 }
-__device__ __forceinline__ int wg_min(int v, u64* sh) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = (u64)(uint32_t)v;
-  __syncthreads();
-  v = INT_MAX;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) v = min(v, (int)(uint32_t)sh[w]);
-  return v;
+template <typename T>
+__device__ __forceinline__ T wg_sum(T v, void* scratch) {
+  T total;
+  wg_scan(v, scratch, total);
+  return total;
 }
-
-// All threads: sum / exclusive prefix over the workgroup in thread order.
-__device__ __forceinline__ u64 wg_scan(u64 v, u64* sh, u64& total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  u64 inc = v;
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const u64 up = __shfl_up(inc, o);
-    if (lane >= o) inc += up;
-  }
+__device__ __forceinline__ float wg_max(float v, void* scratch) {
+  float* sh = static_cast<float*>(scratch);
+  v = wave_max(v);
   __syncthreads();
-  if (lane == 63) sh[wave] = inc;
+  sh[threadIdx.x >> 6] = v;
   __syncthreads();
-  u64 base = 0, t = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w == wave) base = t;
-    t += sh[w];
-  }
-  total = t;
-  return base + inc - v;
+  return wave_max(sh[threadIdx.x & (kWaves - 1)]);
+}
+// (ints below 2^24 and INT_MAX, as floats are exact up to there)
+__device__ __forceinline__ int wg_min(int v, void* scratch) {
+  const float m = wg_max(v == INT_MAX ? -INFINITY : -(float)v, scratch);
+  return m == -INFINITY ? INT_MAX : (int)-m;
 }
 
-// f(j, l[4]) for every four tokens j .. j+3 of the row, thread t of each
-// round the four at round * 4096 + 4 t; tokens past the end are -inf.
+// f(round, j, l[4]) for every four tokens j .. j+3 of the row, thread t of each round
+// the four at round * 4096 + 4 t; tokens past the end are -inf.  Four rounds' loads
+// are in flight together: one workgroup reads a row of 152064 in 12 us instead of 30.
 template <typename F>
 __device__ __forceinline__ void each4(const SampleK& a, const float* __restrict__ row, F f) {
+  constexpr int NR = 4;
   const int rounds = (a.V + 4 * kThreads - 1) / (4 * kThreads);
-  for (int r = 0; r < rounds; ++r) {
-    const int j = r * 4 * kThreads + 4 * (int)threadIdx.x;
-    float l[4];
-    if (a.vec && j + 3 < a.V) {
-      const f32x4 q = *reinterpret_cast<const f32x4*>(row + j);
+  for (int r = 0; r < rounds; r += NR) {
+    f32x4 l[NR];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) l[e] = q[e];
-    } else {
+    for (int i = 0; i < NR; ++i) {
+      const int j = ((r + i) * kThreads + (int)threadIdx.x) * 4;
+      if (a.vec && j + 3 < a.V)
+        l[i] = *reinterpret_cast<const f32x4*>(row + j);
+      else
 #pragma unroll
-      for (int e = 0; e < 4; ++e) l[e] = j + e < a.V ? row[j + e] : -INFINITY;
+        for (int e = 0; e < 4; ++e) l[i][e] = j + e < a.V ? row[j + e] : -INFINITY;
     }
-    f(r, j, l);
+#pragma unroll
+    for (int i = 0; i < NR; ++i)
+      if (r + i < rounds) f(r + i, ((r + i) * kThreads + (int)threadIdx.x) * 4, l[i]);
   }
 }
 
 // Sorts list[0..n) ascending, n a power of two (two barriers a step, 10 to 78 steps).
-__device__ void bitonic_sort(u64* list, int n) {
+__device__ __forceinline__ void bitonic_sort(u64* list, int n) {
   for (int k = 2; k <= n; k <<= 1)
     for (int j = k >> 1; j > 0; j >>= 1) {
       __syncthreads();
@@ -285,28 +300,23 @@ __device__ void bitonic_sort(u64* list, int n) {
   __syncthreads();
 }
 
-// Sorts list[0..n) ascending, keys distinct; list has room for kCap.  Up to kRankMax
-// keys each finds its place by counting the smaller ones (n^2 / 1024 comparisons a
-// thread, three barriers: 0.3 us at 256 keys where the network takes 5), more go
-// through the network, padded to a power of two.
-constexpr int kRankMax = 1024;
-__device__ void sort_list(u64* list, int n) {
+// Sorts list[0..n) ascending, n <= kShort, keys distinct, list with room for 3 kShort:
+// each key finds its place by counting the smaller ones (n^2 / 1024 comparisons a thread
+// and four barriers: 256 keys in 0.3 us where the network takes 5).  Thread t returns with
+// key t (of n).
+__device__ __forceinline__ u64 rank_sort(u64* list, int n) {
   const int tid = threadIdx.x;
   int n2 = kWave;
   while (n2 < n) n2 <<= 1;
-  __syncthreads();
-  for (int i = n + tid; i < n2; i += kThreads) list[i] = ~0ull;
-  if (n > kRankMax) {
-    bitonic_sort(list, n2);
-    return;
-  }
-  int* rank = reinterpret_cast<int*>(list + 2 * kRankMax);
+  int* rank = reinterpret_cast<int*>(list + 2 * kShort);
+  if (tid >= n && tid < n2) list[tid] = ~0ull;
   rank[tid] = 0;
   __syncthreads();
   const int parts = kThreads / n2, i = tid & (n2 - 1), part = tid / n2, per = n2 / parts >= 2 ? n2 / parts : 2;
   const u64 x = list[i];
   int cnt = 0;
   const ulonglong2* pairs = reinterpret_cast<const ulonglong2*>(list);
+#pragma unroll 4
   for (int j = part * per; j < min((part + 1) * per, n2); j += 2) {
     const ulonglong2 y = pairs[j / 2];
     cnt += (y.x < x) + (y.y < x);
@@ -316,10 +326,16 @@ __device__ void sort_list(u64* list, int n) {
     __syncthreads();
     cnt = rank[i];
   }
-  if (part == 0 && i < n) list[kRankMax + cnt] = x;
+  if (part == 0 && i < n) list[kShort + cnt] = x;
   __syncthreads();
-  if (tid < n) list[tid] = list[kRankMax + tid];
-  __syncthreads();
+  return tid < n ? list[kShort + tid] : ~0ull;
+}
+// The same in place for n <= kCap, by a network: for the long way.
+__device__ __forceinline__ void sort_list(u64* list, int n) {
+  int n2 = 2;
+  while (n2 < n) n2 <<= 1;
+  for (int i = n + threadIdx.x; i < n2; i += kThreads) list[i] = ~0ull;
+  bitonic_sort(list, n2);
 }
 
 struct RadixOut {
@@ -340,7 +356,7 @@ __device__ __forceinline__ int d_bin(float d) {
 // Radix search: the last token, in order, at which the count reaches k (by_mass
 // false) or the mass reaches `target`; finite logits only.
 template <typename W>
-__device__ RadixOut radix_search(const SampleK& a, const float* row, Shared& sh, bool by_mass, u64 target, W weight) {
+__device__ __forceinline__ RadixOut radix_search(const SampleK& a, const float* row, Shared& sh, bool by_mass, u64 target, W weight) {
   uint32_t prefix = 0, mask = 0;
   u64 before = 0, mass_before = 0;  // of the tokens above the current prefix: count (or mass), mass
   uint32_t ties = 0;
@@ -354,7 +370,7 @@ __device__ RadixOut radix_search(const SampleK& a, const float* row, Shared& sh,
       sh.h.count[i] = 0;
     }
     __syncthreads();
-    each4(a, row, [&](int, int, const float(&l)[4]) {
+    each4(a, row, [&](int, int, const f32x4& l) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const uint32_t k = order_key(l[e]);
@@ -406,17 +422,17 @@ __device__ RadixOut radix_search(const SampleK& a, const float* row, Shared& sh,
 }
 
 // Index of the need-th (from 1) token with logit tau, in index order.
-__device__ int nth_equal(const SampleK& a, const float* row, Shared& sh, float tau, uint32_t need) {
+__device__ __forceinline__ int nth_equal(const SampleK& a, const float* row, Shared& sh, float tau, uint32_t need) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   __syncthreads();
   for (int i = threadIdx.x; i < kMaxTiles; i += kThreads) sh.tsum[i] = 0;
   __syncthreads();
-  each4(a, row, [&](int r, int, const float(&l)[4]) {
+  each4(a, row, [&](int r, int, const f32x4& l) {
     int c = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) c += l[e] == tau;
-    for (int o = 32; o > 0; o >>= 1) c += __shfl_xor(c, o);
-    if (lane == 0) sh.tsum[r * kWaves + wave] = c;
+    c = wave_scan(c);
+    if (lane == 63) sh.tsum[r * kWaves + wave] = c;
   });
   __syncthreads();
   u64 tot;
@@ -432,11 +448,7 @@ __device__ int nth_equal(const SampleK& a, const float* row, Shared& sh, float t
   if (wave == 0) {
     int c = 0, j = tile * kTile + 4 * lane;
     for (int e = 0; e < 4; ++e) c += j + e < a.V && row[j + e] == tau;
-    int inc = c;
-    for (int o = 1; o < kWave; o <<= 1) {
-      const int up = __shfl_up(inc, o);
-      if (lane >= o) inc += up;
-    }
+    const int inc = wave_scan(c);
     if (inc - c < rest && rest <= inc) {
       int left = rest - (inc - c);
       for (int e = 0; e < 4; ++e)
@@ -449,9 +461,11 @@ __device__ int nth_equal(const SampleK& a, const float* row, Shared& sh, float t
 
 // The tokens that `in` takes from the tiles whose max is at least `cut`, to sh.list in
 // no order, as sort keys (logit descending, index); returns their number (more than
-// kCap: the list is cut off).
+// kCap: the list is cut off).  few: with every one of 128 tiles or more at or above the
+// cut, some ln(tiles) or more tokens a tile are, too many for the short way: none are
+// read, and the number is kCap + 1.
 template <typename F>
-__device__ int collect(const SampleK& a, const float* row, Shared& sh, float cut, F in) {
+__device__ __forceinline__ int collect(const SampleK& a, const float* row, Shared& sh, float cut, bool few, F in) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   __syncthreads();
   if (tid < 2) sh.out32[tid] = 0;
@@ -460,6 +474,7 @@ __device__ int collect(const SampleK& a, const float* row, Shared& sh, float cut
     if (sh.tmax[t] >= cut && sh.tmax[t] > -INFINITY) sh.tiles[atomicAdd(&sh.out32[0], 1)] = (uint16_t)t;
   __syncthreads();
   const int nq = sh.out32[0];
+  if (few && nq == a.ntile && nq >= 128) return kCap + 1;
   constexpr int NI = 4;  // tiles in flight per wave
   for (int i = wave; i < nq; i += NI * kWaves) {
     f32x4 l[NI];
@@ -514,6 +529,39 @@ __device__ __forceinline__ int find_bin(u64 b0, u64 b1, u64 want, Shared& sh, u6
 
 __device__ __forceinline__ float list_logit(u64 v) { return key_logit(~(uint32_t)(v >> 32)); }
 
+// Sorts the n listed tokens; of them, the last in order at which their number, or the
+// mass from `before` on, reaches `want` (the very last if none does), and the mass up to it.
+template <typename W>
+__device__ __forceinline__ u64 last_listed(Shared& sh, int n, u64 want, bool by_mass, u64 before, float& tau, int& tau_idx,
+                                           W weight) {
+  const int tid = threadIdx.x;
+  sort_list(sh.list, n);
+  u64 w[4], ls = 0, all;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int i = 4 * tid + e;
+    w[e] = i < n ? weight(list_logit(sh.list[i])) : 0;
+    ls += w[e];
+  }
+  u64 run = before + wg_scan(ls, sh.red, all), upto = 0;
+  int at = INT_MAX;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int i = 4 * tid + e;
+    run += w[e];
+    if (i < n && at == INT_MAX && ((by_mass ? run >= want : (u64)i + 1 >= want) || i == n - 1)) {
+      at = i;
+      upto = run;
+    }
+  }
+  const int last = wg_min(at, sh.red);
+  if (at == last) sh.out64[1] = upto;
+  __syncthreads();
+  tau = list_logit(sh.list[last]);
+  tau_idx = (int)(uint32_t)sh.list[last];
+  return sh.out64[1];
+}
+
 // One workgroup per row.
 __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
   __shared__ Shared sh;
@@ -526,10 +574,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
     m = fmaxf(m, sh.tmax[t]);
     if (s.mass) sh.tmass[t] = a.tmass[(size_t)r * a.ntile + t];
   }
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  if (lane == 0) sh.red[wave] = __float_as_uint(m);
-  __syncthreads();
-  for (int w = 0; w < kWaves; ++w) m = fmaxf(m, __uint_as_float((uint32_t)sh.red[w]));
+  m = wg_max(m, sh.red);
   if (!s.ok || !(m > -INFINITY && m < INFINITY)) {  // (a NaN shows as +inf)
     if (tid == 0) {
       a.tokens[r] = -1;
@@ -573,14 +618,14 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
       sh.tmass[t] = sh.tmax[t] > -INFINITY ? sh.tmass[t] * weight(sh.tmax[t]) : 0.0;
       mass += sh.tmass[t];
     }
-    mass = wg_sum(mass, sh.redd);
+    mass = wg_sum(mass, sh.red);
   }
 
   if (!s.by_count && !s.by_mass && s.Q == 0.f) {
     // no truncation: the tile in which the running sum passes u * total, then the token
     const double m0 = 2 * tid < a.ntile ? sh.tmass[2 * tid] : 0.0, m1 = 2 * tid + 1 < a.ntile ? sh.tmass[2 * tid + 1] : 0.0;
     double total;
-    const double base = wg_scan(m0 + m1, sh.redd, total);
+    const double base = wg_scan(m0 + m1, sh.red, total);
     const double t = (double)s.u * total;
     int tile = base + m0 > t && m0 > 0.0 ? 2 * tid : base + (m0 + m1) > t && m1 > 0.0 ? 2 * tid + 1 : INT_MAX;
     tile = wg_min(tile, sh.red);
@@ -588,9 +633,9 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
       int last = m1 > 0.0 ? 2 * tid + 1 : m0 > 0.0 ? 2 * tid : -1;
       tile = -wg_min(-last, sh.red);
     }
-    if (tid == tile / 2) sh.redd[0] = base + (tile & 1 ? m0 : 0.0);
+    if (tid == tile / 2) sh.out64[0] = __double_as_longlong(base + (tile & 1 ? m0 : 0.0));
     __syncthreads();
-    const double before = sh.redd[0];
+    const double before = __longlong_as_double(sh.out64[0]);
     if (wave == 0) {
       const f32x4 l = tile_quad(a, row, tile);
       double w[4], ls = 0.0;
@@ -599,12 +644,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
         w[e] = weight(l[e]);
         ls += w[e];
       }
-      double inc = ls;
-      for (int o = 1; o < kWave; o <<= 1) {
-        const double up = __shfl_up(inc, o);
-        if (lane >= o) inc += up;
-      }
-      double run = before + (inc - ls);
+      double run = before + (wave_scan(ls) - ls);
       int at = INT_MAX, last = -1;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -645,8 +685,8 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
   constexpr float kGuess[kGuesses] = {-5.f, -8.f, -12.f, -16.f, -24.f};  // log2 of the weight
   int n = 0;
   bool listed = false;
-  double target = 0.0;
-  for (int round = 0; !listed; ++round) {
+  double target = INFINITY;
+  for (int round = 0; !listed && !(s.by_count && s.K > kShort); ++round) {
     if (s.by_count) {
       // ranks of the tile maxima: K, or with fewer tiles 1/2, 3/4 and all of them
       const int rank = s.K <= a.ntile ? s.K : round == 0 ? (a.ntile + 1) / 2 : round == 1 ? (3 * a.ntile + 3) / 4 : a.ntile;
@@ -656,169 +696,167 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
       cut = !s.by_mass ? (float)(md + (log2(mind) - 1e-6) / s.scale) : round < kGuesses ? (float)(md + kGuess[round] / s.scale) : -INFINITY;
       cut = fminf(cut, m) - fabsf(cut) * 0x1p-22f;
     }
-    n = collect(a, row, sh, cut, [&](float l) { return l >= cut; });
-    if (n > kCap) break;
+    n = collect(a, row, sh, cut, !s.by_count, [&](float l) { return l >= cut; });
+    if (n > kShort) break;
     if (s.by_count) {
       if (n < s.K && cut > -INFINITY) {
         if (s.K <= a.ntile || round >= 2) break;  // (more than one token per tile is kept)
         continue;
       }
     } else if (s.by_mass) {
-      double w = 0.0;
-      for (int i = tid; i < n; i += kThreads) w += weight(list_logit(sh.list[i]));
-      w = wg_sum(w, sh.redd);
       target = (double)s.P * mass;
+      const double w = wg_sum(tid < n ? weight(list_logit(sh.list[tid])) : 0.0, sh.red);
       if (w < target && cut > -INFINITY) continue;
     }
-    sort_list(sh.list, n);
     listed = true;
   }
   if (listed) {
-    const int kk = min(s.K, n);
-    // prefix sums of the weights, four tokens a thread
-    double w[4], ls = 0.0, tot;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int i = 4 * tid + e;
-      w[e] = i < kk ? weight(list_logit(sh.list[i])) : 0.0;
-      ls += w[e];
-    }
-    double run = wg_scan(ls, sh.redd, tot);
-    if (!s.by_mass) target = INFINITY;
-    else if (s.by_count) target = (double)s.P * tot;
-    // kept: i < kk, the sum before it below the target (or i = 0), w >= min_p
-    int cnt = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int i = 4 * tid + e;
-      cnt += i < kk && (i == 0 || run < target) && w[e] >= mind;
-      run += w[e];
-    }
-    u64 all;
-    wg_scan((u64)cnt, sh.red, all);
-    const int L = (int)all;
-    const u64 last = sh.list[L - 1];
-    // the kept tokens in index order
-    __syncthreads();
-    for (int i = tid; i < L; i += kThreads) sh.list[i] = (sh.list[i] << 32) | (sh.list[i] >> 32);
-    sort_list(sh.list, L);
-    ls = 0.0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int i = 4 * tid + e;
-      w[e] = i < L ? weight(key_logit(~(uint32_t)sh.list[i])) : 0.0;
-      ls += w[e];
-    }
+    // sorted by rank the list says what is kept, sorted by index what is drawn
+    int L = min(s.K, n), at = 0;
+    float tau = 0.f;
+    int tau_idx = 0;
     double total;
-    run = wg_scan(ls, sh.redd, total);
-    const double t = (double)s.u * total;
-    int at = INT_MAX;  // the first whose running sum passes t; the last if rounding leaves none
-#pragma unroll
-    for (int e = 3; e >= 0; --e) {
-      double incl = run;
-      for (int f = 0; f <= e; ++f) incl += w[f];
-      if (4 * tid + e < L && incl > t) at = 4 * tid + e;
+#pragma unroll 1
+    for (int by_index = 0; by_index < 2; ++by_index) {
+      u64 x = rank_sort(sh.list, n);
+      if (by_index) x = (x << 32) | (x >> 32);
+      const double w = tid < L ? weight(list_logit(x)) : 0.0, run = wg_scan(w, sh.red, total);
+      if (by_index) {  // the first whose running sum passes u of the total; the last if rounding leaves none
+        at = min(wg_min(run + w > (double)s.u * total && tid < L ? tid : INT_MAX, sh.red), L - 1);
+        if (tid == at) {
+          a.tokens[r] = (int)(uint32_t)x;
+          a.head[r] = {1.0 / total, m, tau, tau_idx};
+        }
+      } else {  // kept: the first K, the sum before below the target (or the first of all), w >= min_p
+        if (s.by_mass && s.by_count) target = (double)s.P * total;
+        L = __syncthreads_count(tid < L && (tid == 0 || run < target) && w >= mind);
+        if (tid < L) sh.list[tid] = (x << 32) | (x >> 32);
+        if (tid == L - 1) sh.out64[0] = x;
+        n = L;
+        __syncthreads();
+        tau = list_logit(sh.out64[0]);
+        tau_idx = (int)(uint32_t)sh.out64[0];
+      }
     }
-    at = min(wg_min(at, sh.red), L - 1);
-    done((int)(uint32_t)(sh.list[at] >> 32), list_logit(last), (int)(uint32_t)last, total);
     return;
   }
 
   // The long way: a histogram of the whole row over d_bin finds the bin of the last
   // token, a list of that bin's tokens the token; a bin that holds more than the list
-  // (equal logits by the thousand) is searched by the logits' bits.
+  // (equal logits by the thousand) is searched by the logits' bits.  With top-p alone the
+  // histogram is of fp32 weights (64-bit ones for every token cost twice the pass): it is
+  // good for 2^-16 of what it sums, so that all bins which may hold the last token are
+  // listed, and the pass that sums the others exactly finds it among them.
   auto weight44 = [&](float l) { return fixed44(weight(l)); };
   float tau = -INFINITY;
   int tau_idx = V;
-  if (s.by_count || s.by_mass) {
-    __syncthreads();
-    for (int i = tid; i < kBins; i += kThreads) {
-      sh.h.mass[i] = 0;
-      sh.h.count[i] = 0;
-    }
-    __syncthreads();
-    each4(a, row, [&](int, int, const float(&l)[4]) {
+  auto kept = [&](float l, int j) { return l != -INFINITY && (l > tau || (l == tau && j <= tau_idx)); };
+  const u64 want_mass = (u64)ceil((double)s.P * (mass * 0x1p44));
+#pragma unroll 1
+  for (bool open = s.by_mass && !s.by_count;; open = false) {  // open: the last token is found under the last pass
+    int bin_lo = 0, bin_hi = -1;
+    if (s.by_count || s.by_mass) {
+      __syncthreads();
+      for (int i = tid; i < kBins; i += kThreads) {
+        sh.h.mass[i] = 0;
+        sh.h.count[i] = 0;
+      }
+      __syncthreads();
+      const float scale = (float)s.scale;
+      each4(a, row, [&](int, int, const f32x4& l) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (l[e] != -INFINITY) {
-          const int bin = d_bin(m - l[e]);
-          if (s.by_count) atomicAdd(&sh.h.count[bin], 1u);
-          if (s.by_mass) {
-            const u64 w = weight44(l[e]);
-            if (w) atomicAdd(&sh.h.mass[bin], w);
+        for (int e = 0; e < 4; ++e)
+          if (l[e] != -INFINITY) {
+            const int bin = d_bin(m - l[e]);
+            if (open) {
+              const float w = __builtin_amdgcn_exp2f((l[e] - m) * scale);
+              if (w > 0x1p-45f) atomicAdd(&sh.h.mass[bin], (u64)(w * 0x1p44f));
+            } else {
+              atomicAdd(&sh.h.count[bin], 1u);
+              if (s.by_mass) {
+                const u64 w = weight44(l[e]);
+                if (w) atomicAdd(&sh.h.mass[bin], w);
+              }
+            }
+          }
+      });
+      __syncthreads();
+      const u64 c0 = sh.h.count[2 * tid], c1 = sh.h.count[2 * tid + 1], m0 = sh.h.mass[2 * tid], m1 = sh.h.mass[2 * tid + 1];
+      u64 ctot, mtot;
+      const u64 x1 = wg_scan(m0 + m1, sh.red, mtot) + m0, x2 = x1 + m1;
+      wg_scan(c0 + c1, sh.red, ctot);
+      if (open) {
+        const u64 slack = 2 * (u64)V;
+        auto above = [&](u64 x) { return x + (x >> 16) + slack >= want_mass; };
+        auto below = [&](u64 x) { return x >= (x >> 16) + slack + want_mass; };
+        bin_lo = wg_min(above(x1) ? 2 * tid : above(x2) ? 2 * tid + 1 : INT_MAX, sh.red);
+        bin_hi = min(wg_min(below(x1) ? 2 * tid : below(x2) ? 2 * tid + 1 : INT_MAX, sh.red), kBins - 1);
+      } else {
+        // the last token at which the count, then the mass, reaches `want`
+        u64 have = mtot;  // the mass up to it
+#pragma unroll 1
+        for (int by_mass = !s.by_count; by_mass <= s.by_mass; ++by_mass) {
+          u64 want = by_mass ? s.by_count ? (u64)ceil((double)s.P * (double)have) : want_mass : (u64)s.K, before, mbefore;
+          want = min(max(want, (u64)1), by_mass ? mtot : ctot);
+          const int bin = find_bin(by_mass ? m0 : c0, by_mass ? m1 : c1, want, sh, before);
+          wg_scan((2 * tid < bin ? m0 : 0) + (2 * tid + 1 < bin ? m1 : 0), sh.red, mbefore);
+          const int nb = collect(a, row, sh, bin_floor(m, bin), false, [&](float l) { return d_bin(m - l) == bin; });
+          if (nb > kCap) {
+            const RadixOut x = radix_search(a, row, sh, by_mass, want, weight44);
+            tau = key_logit(x.key);
+            tau_idx = nth_equal(a, row, sh, tau, x.need);
+            have = x.mass;
+          } else {
+            have = last_listed(sh, nb, by_mass ? want : want - before, by_mass, mbefore, tau, tau_idx,
+                               [&](float l) { return s.by_mass ? weight44(l) : 0; });
           }
         }
-    });
+      }
+    }
+    // kept weights of the tiles
     __syncthreads();
-    const u64 c0 = sh.h.count[2 * tid], c1 = sh.h.count[2 * tid + 1], m0 = sh.h.mass[2 * tid], m1 = sh.h.mass[2 * tid + 1];
-    u64 ctot, mtot;
-    wg_scan(c0 + c1, sh.red, ctot);
-    wg_scan(m0 + m1, sh.red, mtot);
-    // the last token at which the count (or the mass) reaches `want`, and the mass up to it
-    auto search = [&](bool by_mass, u64 want) {
-      u64 before, mbefore = 0;
-      const int bin = by_mass ? find_bin(m0, m1, want, sh, before) : find_bin(c0, c1, want, sh, before);
-      if (by_mass) {
-        mbefore = before;
-      } else if (s.by_mass) {  // the mass before that bin
-        wg_scan((2 * tid < bin ? m0 : 0) + (2 * tid + 1 < bin ? m1 : 0), sh.red, mbefore);
-      }
-      const int nb = collect(a, row, sh, bin_floor(m, bin), [&](float l) { return d_bin(m - l) == bin; });
-      if (nb > kCap) {
-        const RadixOut x = radix_search(a, row, sh, by_mass, want, weight44);
-        tau = key_logit(x.key);
-        tau_idx = nth_equal(a, row, sh, tau, x.need);
-        return x.mass;
-      }
-      sort_list(sh.list, nb);
-      u64 w[4], ls = 0, all;
+    for (int i = tid; i < kMaxTiles; i += kThreads) sh.tsum[i] = 0;
+    if (tid == 0) sh.out32[1] = 0;
+    __syncthreads();
+    u64 all = 0;
+    each4(a, row, [&](int rd, int j, const f32x4& l) {
+      u64 sum = 0;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int i = 4 * tid + e;
-        w[e] = i < nb && (by_mass || s.by_mass) ? weight44(list_logit(sh.list[i])) : 0;
-        ls += w[e];
-      }
-      u64 run = mbefore + wg_scan(ls, sh.red, all);
-      int at = INT_MAX;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int i = 4 * tid + e;
-        const bool hit = i < nb && (by_mass ? run < want && want <= run + w[e] : before + (u64)i + 1 == want);
-        run += w[e];
-        if (hit) {
-          at = i;
-          sh.out64[1] = run;
+        const int bin = open ? l[e] != -INFINITY ? d_bin(m - l[e]) : kBins : 0;
+        if (open ? bin < bin_lo : kept(l[e], j + e)) {
+          const double w = weight(l[e]);
+          const u64 f = fixed44(w);
+          all += f;
+          if (w >= mind) sum += f;
+        }
+        if (open) {
+          const bool take = bin >= bin_lo && bin <= bin_hi;
+          const u64 who = __ballot(take);
+          if (who) {
+            int at = 0;
+            if (lane == 0) at = atomicAdd(&sh.out32[1], __popcll(who));
+            at = __builtin_amdgcn_readfirstlane(at) + __popcll(who & ((1ull << lane) - 1));
+            if (take && at < kCap) sh.list[at] = ((u64)~order_key(l[e]) << 32) | (uint32_t)(j + e);
+          }
         }
       }
-      at = min(wg_min(at, sh.red), nb - 1);
-      tau = list_logit(sh.list[at]);
-      tau_idx = (int)(uint32_t)sh.list[at];
-      return sh.out64[1];
-    };
-    u64 have = mtot;
-    if (s.by_count) have = search(false, min((u64)s.K, ctot));
-    // (by mass alone: of the tiles' sums, as on the short way)
-    if (s.by_mass) {
-      const double of = s.by_count ? (double)have : mass * 0x1p44;
-      search(true, min(max((u64)ceil((double)s.P * of), (u64)1), mtot));
+      sum = wave_scan(sum);
+      if (lane == 63) sh.tsum[rd * kWaves + wave] = sum;
+    });
+    if (!open) break;
+    all = wg_sum(all, sh.red);
+    const int nb = sh.out32[1];
+    if (nb > kCap) continue;
+    last_listed(sh, nb, want_mass, true, all, tau, tau_idx, weight44);
+    for (int i = tid; i < nb; i += kThreads) {
+      const u64 x = sh.list[i];
+      const int j = (int)(uint32_t)x;
+      const double w = weight(list_logit(x));
+      if (kept(list_logit(x), j) && w >= mind) atomicAdd(&sh.tsum[j / kTile], fixed44(w));
     }
+    break;
   }
-  auto kept = [&](float l, int j) { return l != -INFINITY && (l > tau || (l == tau && j <= tau_idx)); };
-  // weights of 256-token tiles, the tile, the token
-  __syncthreads();
-  for (int i = tid; i < kMaxTiles; i += kThreads) sh.tsum[i] = 0;
-  __syncthreads();
-  each4(a, row, [&](int rd, int j, const float(&l)[4]) {
-    u64 sum = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (kept(l[e], j + e)) {
-        const double w = weight(l[e]);
-        if (w >= mind) sum += fixed44(w);
-      }
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-    if (lane == 0) sh.tsum[rd * kWaves + wave] = sum;
-  });
   __syncthreads();
   const u64 s0 = sh.tsum[2 * tid], s1 = sh.tsum[2 * tid + 1];
   u64 total;
@@ -832,22 +870,18 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
   __syncthreads();
   if (wave == 0) {
     const int j = sh.out32[0] * kTile + 4 * lane;
+    const f32x4 l = tile_quad(a, row, sh.out32[0]);
     u64 w[4], ls = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       w[e] = 0;
-      if (j + e < V && kept(row[j + e], j + e)) {
-        const double x = weight(row[j + e]);
+      if (kept(l[e], j + e)) {
+        const double x = weight(l[e]);
         if (x >= mind) w[e] = fixed44(x);
       }
       ls += w[e];
     }
-    u64 inc = ls;
-    for (int o = 1; o < kWave; o <<= 1) {
-      const u64 up = __shfl_up(inc, o);
-      if (lane >= o) inc += up;
-    }
-    u64 run = sh.out64[0] + inc - ls;
+    u64 run = sh.out64[0] + wave_scan(ls) - ls;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       if (run <= t && t < run + w[e]) sh.out32[2] = j + e;
