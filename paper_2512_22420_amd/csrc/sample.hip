@@ -33,19 +33,20 @@ namespace {
 
 constexpr int kErrSampling = 32;  // NJ_DEV_BAD_SAMPLING
 constexpr int kThreads = 1024, kWaves = kThreads / kWave;
-constexpr int kBins = 2048;
-constexpr int kShort = 1024;      // tokens that the short way sorts, one a thread
-constexpr int kCap = 4096;        // tokens that the long way lists
+constexpr int kBins = 4096, kBitBins = 2048;
+constexpr int kCap = 4096;        // tokens of a list
 constexpr int kTile = 256;        // tokens per running-sum tile (four per lane of a wave)
 constexpr int kMaxTiles = 2048;   // V <= 524288
 typedef unsigned long long u64;
 
 // exp2(x) for x <= 0 in 64 bits: 2^n (1 + f q(f)), |f| <= 1/2, where q is the polynomial
 // that meets (2^f - 1) / f at the nine Chebyshev points of that interval: relative error
-// below 4e-14.  exp2(0) = 1 exactly, exp2(-inf) = 0.
+// below 4e-14.  exp2(0) = 1 exactly; below 2^-1020 (and at -inf) 2^-1020.  n is rounded by
+// adding 1.5 * 2^52, whose low word it leaves it in, and goes to the exponent's bits:
+// additions only, 64-bit roundings and conversions being slow.
 __device__ __forceinline__ double exp2_64(double x) {
-  x = fmax(x, -2000.0);
-  const double n = rint(x), f = x - n;
+  x = fmax(x, -1020.0);
+  const double big = x + 0x1.8p52, f = x - (big - 0x1.8p52);
   double p = 0x1.b63871ee00eb4p-24;
   p = fma(p, f, 0x1.63d13637e6140p-20);
   p = fma(p, f, 0x1.ffcb952643063p-17);
@@ -55,7 +56,8 @@ __device__ __forceinline__ double exp2_64(double x) {
   p = fma(p, f, 0x1.c6b08d7047e8ap-5);
   p = fma(p, f, 0x1.ebfbdff823cedp-3);
   p = fma(p, f, 0x1.62e42fefa39efp-1);
-  return ldexp(fma(p, f, 1.0), (int)n);
+  p = fma(p, f, 1.0);
+  return __hiloint2double(__double2hiint(p) + (int)((uint32_t)__double2loint(big) << 20), __double2loint(p));
 }
 __device__ __forceinline__ u64 fixed44(double w) { return (u64)(w * 0x1p44 + 0.5); }
 
@@ -209,9 +211,10 @@ __global__ __launch_bounds__(256) void sample_tiles_kernel(SampleK a) {
 
 struct Shared {
   union {
+    uint32_t bins[2 * kBins];  // two copies, for even and odd lanes
     struct {
-      u64 mass[kBins];
-      uint32_t count[kBins];
+      u64 mass[kBitBins];
+      uint32_t count[kBitBins];
     } h;
     __attribute__((aligned(16))) u64 list[kCap];
   };
@@ -260,82 +263,92 @@ __device__ __forceinline__ int wg_min(int v, void* scratch) {
 }
 
 // f(round, j, l[4]) for every four tokens j .. j+3 of the row, thread t of each round
-// the four at round * 4096 + 4 t; tokens past the end are -inf.  Four rounds' loads
-// are in flight together: one workgroup reads a row of 152064 in 12 us instead of 30.
+// the four at round * 4096 + 4 t; tokens past the end are -inf.  Four rounds' loads are
+// in flight while the four before are worked on.
 template <typename F>
 __device__ __forceinline__ void each4(const SampleK& a, const float* __restrict__ row, F f) {
   constexpr int NR = 4;
   const int rounds = (a.V + 4 * kThreads - 1) / (4 * kThreads);
+  auto load = [&](int r) {
+    const int j = (r * kThreads + (int)threadIdx.x) * 4;
+    if (a.vec && j + 3 < a.V) return *reinterpret_cast<const f32x4*>(row + j);
+    f32x4 l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) l[e] = j + e < a.V ? row[j + e] : -INFINITY;
+    return l;
+  };
+  f32x4 next[NR];
+#pragma unroll
+  for (int i = 0; i < NR; ++i) next[i] = load(i);
   for (int r = 0; r < rounds; r += NR) {
     f32x4 l[NR];
 #pragma unroll
-    for (int i = 0; i < NR; ++i) {
-      const int j = ((r + i) * kThreads + (int)threadIdx.x) * 4;
-      if (a.vec && j + 3 < a.V)
-        l[i] = *reinterpret_cast<const f32x4*>(row + j);
-      else
+    for (int i = 0; i < NR; ++i) l[i] = next[i];
+    if (r + NR < rounds)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) l[i][e] = j + e < a.V ? row[j + e] : -INFINITY;
-    }
+      for (int i = 0; i < NR; ++i) next[i] = load(r + NR + i);
 #pragma unroll
     for (int i = 0; i < NR; ++i)
       if (r + i < rounds) f(r + i, ((r + i) * kThreads + (int)threadIdx.x) * 4, l[i]);
   }
 }
 
-// Sorts list[0..n) ascending, n a power of two (two barriers a step, 10 to 78 steps).
-__device__ __forceinline__ void bitonic_sort(u64* list, int n) {
-  for (int k = 2; k <= n; k <<= 1)
-    for (int j = k >> 1; j > 0; j >>= 1) {
-      __syncthreads();
-      for (int t = threadIdx.x; t < n / 2; t += kThreads) {
-        const int i = 2 * t - (t & (j - 1)), p = i + j;
-        const u64 x = list[i], y = list[p];
-        if ((x > y) == ((i & k) == 0)) {
-          list[i] = y;
-          list[p] = x;
-        }
-      }
-    }
-  __syncthreads();
-}
-
-// Sorts list[0..n) ascending, n <= kShort, keys distinct, list with room for 3 kShort:
-// each key finds its place by counting the smaller ones (n^2 / 1024 comparisons a thread
-// and four barriers: 256 keys in 0.3 us where the network takes 5).  Thread t returns with
-// key t (of n).
-__device__ __forceinline__ u64 rank_sort(u64* list, int n) {
-  const int tid = threadIdx.x;
+// Sorts list[0..n) ascending, 1 <= n <= kCap, keys distinct.  Up to 256 keys each finds
+// its place by counting the smaller ones; up to 1024 go through a bitonic network with a
+// key a thread, whose partners in the wave meet in registers (45 of its 55 steps); more
+// through one in LDS, two barriers a step.
+__device__ __forceinline__ void sort_list(u64* list, int n) {
+  const int t = threadIdx.x;
   int n2 = kWave;
   while (n2 < n) n2 <<= 1;
-  int* rank = reinterpret_cast<int*>(list + 2 * kShort);
-  if (tid >= n && tid < n2) list[tid] = ~0ull;
-  rank[tid] = 0;
-  __syncthreads();
-  const int parts = kThreads / n2, i = tid & (n2 - 1), part = tid / n2, per = n2 / parts >= 2 ? n2 / parts : 2;
-  const u64 x = list[i];
-  int cnt = 0;
-  const ulonglong2* pairs = reinterpret_cast<const ulonglong2*>(list);
+  for (int i = n + t; i < n2; i += kThreads) list[i] = ~0ull;
+  if (n <= 256) {
+    int* rank = reinterpret_cast<int*>(list + kThreads);
+    if (t < n2) rank[t] = 0;
+    __syncthreads();
+    const int parts = kThreads / n2, i = t & (n2 - 1), per = n2 / parts;
+    const u64 x = list[i];
+    int cnt = 0;
 #pragma unroll 4
-  for (int j = part * per; j < min((part + 1) * per, n2); j += 2) {
-    const ulonglong2 y = pairs[j / 2];
-    cnt += (y.x < x) + (y.y < x);
-  }
-  if (parts > 1) {
+    for (int j = t / n2 * per; j < (t / n2 + 1) * per; ++j) cnt += list[j] < x;
     atomicAdd(&rank[i], cnt);
     __syncthreads();
-    cnt = rank[i];
+    if (t < n) list[rank[t]] = x;
+  } else if (n <= kThreads) {
+    __syncthreads();
+    const bool in = t < n2;  // (whole waves)
+    u64 x = in ? list[t] : 0;
+    for (int k = 2; k <= n2; k <<= 1)
+      for (int j = k >> 1; j > 0; j >>= 1) {
+        u64 y = 0;
+        if (j < kWave) {
+          y = __shfl_xor(x, j);
+        } else {
+          __syncthreads();
+          if (in) list[t] = x;
+          __syncthreads();
+          if (in) y = list[t ^ j];
+        }
+        const bool low = (t & j) == 0, up = (t & k) == 0;
+        x = (x < y) == (low == up) ? x : y;
+      }
+    __syncthreads();
+    if (in) list[t] = x;
+  } else {
+    for (int k = 2; k <= n2; k <<= 1)
+      for (int j = k >> 1; j > 0; j >>= 1) {
+        __syncthreads();
+        for (int p = t; p < n2 / 2; p += kThreads) {
+          const int i = 2 * p - (p & (j - 1));
+          const u64 x = list[i], y = list[i + j];
+          if ((x > y) == ((i & k) == 0)) {
+            list[i] = y;
+            list[i + j] = x;
+          }
+        }
+      }
   }
-  if (part == 0 && i < n) list[kShort + cnt] = x;
   __syncthreads();
-  return tid < n ? list[kShort + tid] : ~0ull;
-}
-// The same in place for n <= kCap, by a network: for the long way.
-__device__ __forceinline__ void sort_list(u64* list, int n) {
-  int n2 = 2;
-  while (n2 < n) n2 <<= 1;
-  for (int i = n + threadIdx.x; i < n2; i += kThreads) list[i] = ~0ull;
-  bitonic_sort(list, n2);
 }
 
 struct RadixOut {
@@ -344,12 +357,12 @@ struct RadixOut {
   u64 mass;        // of the tokens kept
 };
 
-// Bin of d = max - l >= 0: the upper 16 bits of d (8 of exponent, 7 of mantissa)
+// Bin of d = max - l >= 0: the upper 17 bits of d (8 of exponent, 8 of mantissa)
 // from 2^-8 on; smaller ones share bin 0, from 2^8 on the last.  A bin's relative
-// width is 2^-7, so that it holds a few per cent of a broad row at most, whatever the
+// width is 2^-8, so that it holds a per cent or two of a broad row at most, whatever the
 // scale of the logits.
 __device__ __forceinline__ int d_bin(float d) {
-  const int k = (int)(__float_as_uint(d) >> 16) - ((127 - 8) << 7);
+  const int k = (int)(__float_as_uint(d) >> 15) - ((127 - 8) << 8);
   return min(max(k, 0), kBins - 1);
 }
 
@@ -461,11 +474,11 @@ __device__ __forceinline__ int nth_equal(const SampleK& a, const float* row, Sha
 
 // The tokens that `in` takes from the tiles whose max is at least `cut`, to sh.list in
 // no order, as sort keys (logit descending, index); returns their number (more than
-// kCap: the list is cut off).  few: with every one of 128 tiles or more at or above the
-// cut, some ln(tiles) or more tokens a tile are, too many for the short way: none are
-// read, and the number is kCap + 1.
+// kCap: the list is cut off).  Where tokens fall on tiles at random and kCap reach the
+// cut, 1 - exp(-kCap / tiles) of the tiles hold one: with `guess` and more of them, none
+// is read, and kCap + 1 returned.
 template <typename F>
-__device__ __forceinline__ int collect(const SampleK& a, const float* row, Shared& sh, float cut, bool few, F in) {
+__device__ __forceinline__ int collect(const SampleK& a, const float* row, Shared& sh, float cut, bool guess, F in) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   __syncthreads();
   if (tid < 2) sh.out32[tid] = 0;
@@ -474,7 +487,7 @@ __device__ __forceinline__ int collect(const SampleK& a, const float* row, Share
     if (sh.tmax[t] >= cut && sh.tmax[t] > -INFINITY) sh.tiles[atomicAdd(&sh.out32[0], 1)] = (uint16_t)t;
   __syncthreads();
   const int nq = sh.out32[0];
-  if (few && nq == a.ntile && nq >= 128) return kCap + 1;
+  if (guess && nq > (1.f - __expf(-(float)kCap / a.ntile)) * a.ntile + 0.5f) return kCap + 1;
   constexpr int NI = 4;  // tiles in flight per wave
   for (int i = wave; i < nq; i += NI * kWaves) {
     f32x4 l[NI];
@@ -494,7 +507,9 @@ __device__ __forceinline__ int collect(const SampleK& a, const float* row, Share
         if (!who) continue;
         int at = 0;
         if (lane == 0) at = atomicAdd(&sh.out32[1], __popcll(who));
-        at = __builtin_amdgcn_readfirstlane(at) + __popcll(who & ((1ull << lane) - 1));
+        at = __builtin_amdgcn_readfirstlane(at);
+        if (guess && at > kCap) i = nq;  // (too many already)
+        at += __popcll(who & ((1ull << lane) - 1));
         if (take && at < kCap) sh.list[at] = ((u64)~order_key(l[q][e]) << 32) | (uint32_t)(t[q] * kTile + 4 * lane + e);
       }
     }
@@ -503,29 +518,39 @@ __device__ __forceinline__ int collect(const SampleK& a, const float* row, Share
   return sh.out32[1];
 }
 
+// The smallest d of bin b >= 1.
+__device__ __forceinline__ float bin_edge(int b) { return __uint_as_float((uint32_t)(b + ((127 - 8) << 8)) << 15); }
 // A bound from below of the logits whose bin is at most b (see d_bin).
 __device__ __forceinline__ float bin_floor(float m, int b) {
   if (b >= kBins - 1) return -INFINITY;
-  const float x = m - __uint_as_float((uint32_t)(b + 1 + ((127 - 8) << 7)) << 16);
+  const float x = m - bin_edge(b + 1);
   return x - fabsf(x) * 0x1p-22f;
 }
 
-// The bin in which the running sum over the bins passes `want` (1 <= want <= the
-// sum), from each thread's two bins; `before`: the sum before it.
-__device__ __forceinline__ int find_bin(u64 b0, u64 b1, u64 want, Shared& sh, u64& before) {
-  u64 tot;
-  const u64 x0 = wg_scan(b0 + b1, sh.red, tot), x1 = x0 + b0, x2 = x1 + b1;
-  if (x0 < want && want <= x1) {
-    sh.out32[2] = 2 * threadIdx.x;
-    sh.out64[0] = x0;
-  } else if (x1 < want && want <= x2) {
-    sh.out32[2] = 2 * threadIdx.x + 1;
-    sh.out64[0] = x1;
-  }
-  __syncthreads();
-  before = sh.out64[0];
-  return sh.out32[2];
+// This thread's four bins, copies joined, as running sums behind what comes before (x[0]).
+__device__ __forceinline__ void scan_bins(Shared& sh, u64 (&x)[5], u64& all) {
+  const uint4 a = reinterpret_cast<const uint4*>(sh.bins)[threadIdx.x], b = reinterpret_cast<const uint4*>(sh.bins + kBins)[threadIdx.x];
+  const u64 n[4] = {(u64)a.x + b.x, (u64)a.y + b.y, (u64)a.z + b.z, (u64)a.w + b.w};
+  x[0] = wg_scan(n[0] + n[1] + n[2] + n[3], sh.red, all);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i + 1] = x[i] + n[i];
 }
+// The first bin for whose running sum `reached` holds (it holds for all behind it too);
+// INT_MAX if there is none.
+template <typename F>
+__device__ __forceinline__ int first_bin(Shared& sh, const u64 (&x)[5], F reached) {
+  int b = INT_MAX;
+#pragma unroll
+  for (int i = 3; i >= 0; --i)
+    if (reached(x[i + 1])) b = 4 * threadIdx.x + i;
+  return wg_min(b, sh.red);
+}
+__device__ __forceinline__ void clear_bins(Shared& sh) {
+  __syncthreads();
+  for (int i = threadIdx.x; i < kBins / 2; i += kThreads) reinterpret_cast<uint4*>(sh.bins)[i] = uint4{0, 0, 0, 0};
+  __syncthreads();
+}
+__device__ __forceinline__ void add_bin(Shared& sh, float d, uint32_t v) { atomicAdd(&sh.bins[d_bin(d) + (threadIdx.x & 1) * kBins], v); }
 
 __device__ __forceinline__ float list_logit(u64 v) { return key_logit(~(uint32_t)(v >> 32)); }
 
@@ -585,12 +610,6 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
   }
   const double md = m, mind = s.Q;
   auto weight = [&](float l) { return exp2_64(((double)l - md) * s.scale); };
-  auto done = [&](int token, float tau, int tau_idx, double total) {
-    if (tid == 0) {
-      a.tokens[r] = token;
-      a.head[r] = {1.0 / total, m, tau, tau_idx};
-    }
-  };
 
   if (s.greedy) {  // the first tile that holds the max, and its first place there
     int first = INT_MAX;
@@ -608,7 +627,10 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
         if (l[e] == m) at = first * kTile + 4 * lane + e;
     }
     at = wg_min(at, sh.red);
-    done(at, m, at, 1.0);
+    if (tid == 0) {
+      a.tokens[r] = at;
+      a.head[r] = {1.0, m, m, at};
+    }
     return;
   }
 
@@ -621,275 +643,240 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
     mass = wg_sum(mass, sh.red);
   }
 
-  if (!s.by_count && !s.by_mass && s.Q == 0.f) {
-    // no truncation: the tile in which the running sum passes u * total, then the token
-    const double m0 = 2 * tid < a.ntile ? sh.tmass[2 * tid] : 0.0, m1 = 2 * tid + 1 < a.ntile ? sh.tmass[2 * tid + 1] : 0.0;
-    double total;
-    const double base = wg_scan(m0 + m1, sh.red, total);
-    const double t = (double)s.u * total;
-    int tile = base + m0 > t && m0 > 0.0 ? 2 * tid : base + (m0 + m1) > t && m1 > 0.0 ? 2 * tid + 1 : INT_MAX;
-    tile = wg_min(tile, sh.red);
-    if (tile == INT_MAX) {  // rounding: the last tile with any weight
-      int last = m1 > 0.0 ? 2 * tid + 1 : m0 > 0.0 ? 2 * tid : -1;
-      tile = -wg_min(-last, sh.red);
-    }
-    if (tid == tile / 2) sh.out64[0] = __double_as_longlong(base + (tile & 1 ? m0 : 0.0));
-    __syncthreads();
-    const double before = __longlong_as_double(sh.out64[0]);
-    if (wave == 0) {
-      const f32x4 l = tile_quad(a, row, tile);
-      double w[4], ls = 0.0;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        w[e] = weight(l[e]);
-        ls += w[e];
-      }
-      double run = before + (wave_scan(ls) - ls);
-      int at = INT_MAX, last = -1;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        run += w[e];
-        const int j = tile * kTile + 4 * lane + e;
-        if (w[e] > 0.0) {
-          if (run > t && at == INT_MAX) at = j;
-          last = j;
-        }
-      }
-      for (int o = 32; o > 0; o >>= 1) {
-        at = min(at, __shfl_xor(at, o));
-        last = max(last, __shfl_xor(last, o));
-      }
-      if (lane == 0) sh.out32[3] = at == INT_MAX ? last : at;
-    }
-    __syncthreads();
-    done(sh.out32[3], -INFINITY, V, total);
-    return;
-  }
+  const bool whole = !s.by_count && !s.by_mass && s.Q == 0.f;  // no truncation: drawn from the tiles' sums
 
-  // A logit that every kept token reaches.  top-k: the bin of the K-th largest tile
-  // max (each tile has a token that large); with fewer tiles than K, some tile's, the
-  // smallest at last.  top-p alone: guesses, lowered while the tokens above fall short
-  // of the target.  min-p alone: its own border (a little below: the test itself decides).
+  // The short way: a logit that every kept token reaches, and the tokens above it.
+  // top-k: some tile's max.  K tokens at least reach the K-th; where tokens fall on tiles
+  // at random, n of them reach the max of rank (1 - exp(-n / tiles)) tiles: a little more
+  // than K is aimed at, then half as much again; the last is the smallest max.
+  // top-p alone: guesses, lowered while the tokens above fall short of the target.
+  // min-p alone: its own border (a little below: the test itself decides).
   float cut = -INFINITY;
-  u64 b0 = 0, b1 = 0;  // this thread's two bins of the tile maxima
-  if (s.by_count) {
-    __syncthreads();
-    for (int i = tid; i < kBins; i += kThreads) sh.h.count[i] = 0;
-    __syncthreads();
-    for (int t = tid; t < a.ntile; t += kThreads) atomicAdd(&sh.h.count[sh.tmax[t] > -INFINITY ? d_bin(m - sh.tmax[t]) : kBins - 1], 1u);
-    __syncthreads();
-    b0 = sh.h.count[2 * tid];
-    b1 = sh.h.count[2 * tid + 1];
-  }
   constexpr int kGuesses = 5;
   constexpr float kGuess[kGuesses] = {-5.f, -8.f, -12.f, -16.f, -24.f};  // log2 of the weight
   int n = 0;
   bool listed = false;
-  double target = INFINITY;
-  for (int round = 0; !listed && !(s.by_count && s.K > kShort); ++round) {
+  for (int round = 0; !listed && !whole && !(s.by_count && s.K > kCap); ++round) {
     if (s.by_count) {
-      // ranks of the tile maxima: K, or with fewer tiles 1/2, 3/4 and all of them
-      const int rank = s.K <= a.ntile ? s.K : round == 0 ? (a.ntile + 1) / 2 : round == 1 ? (3 * a.ntile + 3) / 4 : a.ntile;
-      u64 before;
-      cut = bin_floor(m, find_bin(b0, b1, (u64)rank, sh, before));
+      clear_bins(sh);
+      for (int t = tid; t < a.ntile; t += kThreads) add_bin(sh, m - sh.tmax[t], 1);
+      __syncthreads();
+      u64 x[5], all;
+      scan_bins(sh, x, all);
+      const float aim = (round ? 1.5f : 1.f) * (1.1f * s.K + 4.f * sqrtf((float)s.K));
+      const int rank = round >= 2 ? a.ntile : max((int)ceilf((1.f - __expf(-aim / a.ntile)) * a.ntile), 1);
+      const u64 want = min(rank, min(s.K, a.ntile));
+      cut = bin_floor(m, first_bin(sh, x, [&](u64 x) { return x >= want; }));
     } else {
       cut = !s.by_mass ? (float)(md + (log2(mind) - 1e-6) / s.scale) : round < kGuesses ? (float)(md + kGuess[round] / s.scale) : -INFINITY;
       cut = fminf(cut, m) - fabsf(cut) * 0x1p-22f;
     }
     n = collect(a, row, sh, cut, !s.by_count, [&](float l) { return l >= cut; });
-    if (n > kShort) break;
+    if (n > kCap) break;
     if (s.by_count) {
       if (n < s.K && cut > -INFINITY) {
-        if (s.K <= a.ntile || round >= 2) break;  // (more than one token per tile is kept)
+        if (round >= 2) break;
         continue;
       }
     } else if (s.by_mass) {
-      target = (double)s.P * mass;
-      const double w = wg_sum(tid < n ? weight(list_logit(sh.list[tid])) : 0.0, sh.red);
-      if (w < target && cut > -INFINITY) continue;
+      double w = 0.0;
+      for (int i = tid; i < n; i += kThreads) w += weight(list_logit(sh.list[i]));
+      w = wg_sum(w, sh.red);
+      if (w < (double)s.P * mass && cut > -INFINITY) continue;
     }
     listed = true;
   }
+  float tau = -INFINITY;  // kept: above tau, and equal to it up to tau_idx
+  int tau_idx = -1;
   if (listed) {
-    // sorted by rank the list says what is kept, sorted by index what is drawn
-    int L = min(s.K, n), at = 0;
-    float tau = 0.f;
-    int tau_idx = 0;
-    double total;
-#pragma unroll 1
-    for (int by_index = 0; by_index < 2; ++by_index) {
-      u64 x = rank_sort(sh.list, n);
-      if (by_index) x = (x << 32) | (x >> 32);
-      const double w = tid < L ? weight(list_logit(x)) : 0.0, run = wg_scan(w, sh.red, total);
-      if (by_index) {  // the first whose running sum passes u of the total; the last if rounding leaves none
-        at = min(wg_min(run + w > (double)s.u * total && tid < L ? tid : INT_MAX, sh.red), L - 1);
-        if (tid == at) {
-          a.tokens[r] = (int)(uint32_t)x;
-          a.head[r] = {1.0 / total, m, tau, tau_idx};
-        }
-      } else {  // kept: the first K, the sum before below the target (or the first of all), w >= min_p
-        if (s.by_mass && s.by_count) target = (double)s.P * total;
-        L = __syncthreads_count(tid < L && (tid == 0 || run < target) && w >= mind);
-        if (tid < L) sh.list[tid] = (x << 32) | (x >> 32);
-        if (tid == L - 1) sh.out64[0] = x;
-        n = L;
-        __syncthreads();
-        tau = list_logit(sh.out64[0]);
-        tau_idx = (int)(uint32_t)sh.out64[0];
-      }
+    const int kk = min(s.K, n);
+    for (int i = tid; i < kMaxTiles; i += kThreads) sh.tsum[i] = 0;
+    sort_list(sh.list, n);
+    const bool four = n > kThreads;  // tokens a thread
+    double w[4], ls = 0.0, tot;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = four ? 4 * tid + e : tid;
+      w[e] = i < kk && (four || e == 0) ? weight(list_logit(sh.list[i])) : 0.0;
+      ls += w[e];
     }
-    return;
+    double run = wg_scan(ls, sh.red, tot);
+    // kept: the first K, the sum before below the target (or the first of all), w >= min_p
+    const double target = !s.by_mass ? INFINITY : (double)s.P * (s.by_count ? tot : mass);
+    int cnt = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = four ? 4 * tid + e : tid;
+      if (i < kk && (four || e == 0) && (i == 0 || run < target) && w[e] >= mind) {
+        ++cnt;
+        atomicAdd(&sh.tsum[(uint32_t)sh.list[i] / kTile], fixed44(w[e]));
+      }
+      run += w[e];
+    }
+    const u64 last = sh.list[wg_sum(cnt, sh.red) - 1];
+    tau = list_logit(last);
+    tau_idx = (int)(uint32_t)last;
   }
 
-  // The long way: a histogram of the whole row over d_bin finds the bin of the last
-  // token, a list of that bin's tokens the token; a bin that holds more than the list
-  // (equal logits by the thousand) is searched by the logits' bits.  With top-p alone the
-  // histogram is of fp32 weights (64-bit ones for every token cost twice the pass): it is
-  // good for 2^-16 of what it sums, so that all bins which may hold the last token are
-  // listed, and the pass that sums the others exactly finds it among them.
+  // The long way, in passes over the row.  By count: a histogram over d_bin finds the
+  // bin of the K-th token, a list of that bin the token.  By mass, the mass of what is
+  // left so far being known: a histogram of fp32 weights in 32 bits (64-bit ones, added in
+  // 64 bits, took twice as long) brackets the bin of the last token; the pass that
+  // sums what lies above exactly lists the bracket, and the token is found there.  A list
+  // too small (equal logits by the thousand) is replaced by a search over the logits' bits.
+  auto kept = [&](float l, int j) { return l > tau || (l == tau && j <= tau_idx); };
   auto weight44 = [&](float l) { return fixed44(weight(l)); };
-  float tau = -INFINITY;
-  int tau_idx = V;
-  auto kept = [&](float l, int j) { return l != -INFINITY && (l > tau || (l == tau && j <= tau_idx)); };
-  const u64 want_mass = (u64)ceil((double)s.P * (mass * 0x1p44));
+  enum { kCount, kMass, kBits, kSum, kDraw };
+  bool mass_left = s.by_mass;  // top-p is still to do
+  u64 goal = 0;                // of the search over the bits
 #pragma unroll 1
-  for (bool open = s.by_mass && !s.by_count;; open = false) {  // open: the last token is found under the last pass
-    int bin_lo = 0, bin_hi = -1;
-    if (s.by_count || s.by_mass) {
-      __syncthreads();
-      for (int i = tid; i < kBins; i += kThreads) {
-        sh.h.mass[i] = 0;
-        sh.h.count[i] = 0;
-      }
-      __syncthreads();
-      const float scale = (float)s.scale;
-      each4(a, row, [&](int, int, const f32x4& l) {
+  for (int step = whole || listed ? kDraw : s.by_count ? kCount : s.by_mass ? kMass : kSum; step != kDraw;) {
+    // the mass is at most 2^31 of these units; a token's is cut to whole ones, and good for 2^-17
+    const double unit = 0x1p31 / mass, want = (double)s.P * mass;
+    float near = -1.f, far = INFINITY;  // the bracket: near <= max - l < far
+    if (step == kBits) {
+      const RadixOut x = radix_search(a, row, sh, s.by_mass && !mass_left, goal, weight44);
+      tau = key_logit(x.key);
+      tau_idx = nth_equal(a, row, sh, tau, x.need);
+      step = kSum;
+    }
+    if (step != kSum) {
+      clear_bins(sh);
+      const float scale = (float)s.scale, shift = (float)log2(unit);
+      each4(a, row, [&](int, int j, const f32x4& l) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (l[e] != -INFINITY) {
-            const int bin = d_bin(m - l[e]);
-            if (open) {
-              const float w = __builtin_amdgcn_exp2f((l[e] - m) * scale);
-              if (w > 0x1p-45f) atomicAdd(&sh.h.mass[bin], (u64)(w * 0x1p44f));
-            } else {
-              atomicAdd(&sh.h.count[bin], 1u);
-              if (s.by_mass) {
-                const u64 w = weight44(l[e]);
-                if (w) atomicAdd(&sh.h.mass[bin], w);
-              }
-            }
-          }
+        for (int e = 0; e < 4; ++e) {
+          uint32_t u = l[e] > -INFINITY;
+          if (step == kMass) u = kept(l[e], j + e) ? (uint32_t)__builtin_amdgcn_exp2f(fmaf(l[e] - m, scale, shift)) : 0;
+          if (u) add_bin(sh, m - l[e], u);
+        }
       });
       __syncthreads();
-      const u64 c0 = sh.h.count[2 * tid], c1 = sh.h.count[2 * tid + 1], m0 = sh.h.mass[2 * tid], m1 = sh.h.mass[2 * tid + 1];
-      u64 ctot, mtot;
-      const u64 x1 = wg_scan(m0 + m1, sh.red, mtot) + m0, x2 = x1 + m1;
-      wg_scan(c0 + c1, sh.red, ctot);
-      if (open) {
-        const u64 slack = 2 * (u64)V;
-        auto above = [&](u64 x) { return x + (x >> 16) + slack >= want_mass; };
-        auto below = [&](u64 x) { return x >= (x >> 16) + slack + want_mass; };
-        bin_lo = wg_min(above(x1) ? 2 * tid : above(x2) ? 2 * tid + 1 : INT_MAX, sh.red);
-        bin_hi = min(wg_min(below(x1) ? 2 * tid : below(x2) ? 2 * tid + 1 : INT_MAX, sh.red), kBins - 1);
+      u64 x[5], all;
+      scan_bins(sh, x, all);
+      if (step == kMass) {
+        const u64 lo = (u64)floor(want * unit), hi = (u64)ceil(want * unit);
+        const int first = first_bin(sh, x, [&](u64 x) { return x + (x >> 16) + V >= lo; });
+        const int last = first_bin(sh, x, [&](u64 x) { return x - (x >> 16) > hi; });
+        if (first > 0) near = bin_edge(min(first, kBins - 1));
+        if (last < kBins - 1) far = bin_edge(last + 1);
       } else {
-        // the last token at which the count, then the mass, reaches `want`
-        u64 have = mtot;  // the mass up to it
-#pragma unroll 1
-        for (int by_mass = !s.by_count; by_mass <= s.by_mass; ++by_mass) {
-          u64 want = by_mass ? s.by_count ? (u64)ceil((double)s.P * (double)have) : want_mass : (u64)s.K, before, mbefore;
-          want = min(max(want, (u64)1), by_mass ? mtot : ctot);
-          const int bin = find_bin(by_mass ? m0 : c0, by_mass ? m1 : c1, want, sh, before);
-          wg_scan((2 * tid < bin ? m0 : 0) + (2 * tid + 1 < bin ? m1 : 0), sh.red, mbefore);
-          const int nb = collect(a, row, sh, bin_floor(m, bin), false, [&](float l) { return d_bin(m - l) == bin; });
-          if (nb > kCap) {
-            const RadixOut x = radix_search(a, row, sh, by_mass, want, weight44);
-            tau = key_logit(x.key);
-            tau_idx = nth_equal(a, row, sh, tau, x.need);
-            have = x.mass;
-          } else {
-            have = last_listed(sh, nb, by_mass ? want : want - before, by_mass, mbefore, tau, tau_idx,
-                               [&](float l) { return s.by_mass ? weight44(l) : 0; });
-          }
+        const u64 k = min((u64)s.K, all);  // (fewer finite logits than K)
+        const int bin = first_bin(sh, x, [&](u64 x) { return x >= k; });
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (4 * tid + i == bin) sh.out64[0] = x[i];
+        const int nb = collect(a, row, sh, bin_floor(m, bin), false, [&](float l) { return d_bin(m - l) == bin; });
+        if (nb > kCap) {
+          step = kBits;
+          goal = k;
+          continue;
         }
+        last_listed(sh, nb, k - sh.out64[0], false, 0, tau, tau_idx, [](float) { return (u64)0; });
+        step = kSum;
       }
     }
-    // kept weights of the tiles
+    // the sums of the tiles: of what is kept, or of what lies above the bracket
+    const bool open = step == kMass;
+    const double least = !open && mass_left ? 0.0 : mind;  // (top-p is of what top-k keeps, before min-p)
     __syncthreads();
     for (int i = tid; i < kMaxTiles; i += kThreads) sh.tsum[i] = 0;
     if (tid == 0) sh.out32[1] = 0;
     __syncthreads();
-    u64 all = 0;
     each4(a, row, [&](int rd, int j, const f32x4& l) {
-      u64 sum = 0;
+      double sum = 0.0;
+      bool any = false;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int bin = open ? l[e] != -INFINITY ? d_bin(m - l[e]) : kBins : 0;
-        if (open ? bin < bin_lo : kept(l[e], j + e)) {
-          const double w = weight(l[e]);
-          const u64 f = fixed44(w);
-          all += f;
-          if (w >= mind) sum += f;
-        }
-        if (open) {
-          const bool take = bin >= bin_lo && bin <= bin_hi;
-          const u64 who = __ballot(take);
-          if (who) {
-            int at = 0;
-            if (lane == 0) at = atomicAdd(&sh.out32[1], __popcll(who));
-            at = __builtin_amdgcn_readfirstlane(at) + __popcll(who & ((1ull << lane) - 1));
-            if (take && at < kCap) sh.list[at] = ((u64)~order_key(l[e]) << 32) | (uint32_t)(j + e);
+        const float d = m - l[e];
+        const bool k = kept(l[e], j + e);
+        any |= k && !(d < near) && d < far;
+        const double w = weight(l[e]);
+        // (where w < min_p above the bracket, nothing in it is kept either, so that the sum may lack these)
+        if (k && (!open || d < near) && w >= least) sum += w;
+      }
+      if (open && __any(any)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float d = m - l[e];
+          if (kept(l[e], j + e) && !(d < near) && d < far) {
+            const int at = atomicAdd(&sh.out32[1], 1);
+            if (at < kCap) sh.list[at] = ((u64)~order_key(l[e]) << 32) | (uint32_t)(j + e);
           }
         }
       }
       sum = wave_scan(sum);
-      if (lane == 63) sh.tsum[rd * kWaves + wave] = sum;
+      if (lane == 63) sh.tsum[rd * kWaves + wave] = fixed44(sum);
     });
-    if (!open) break;
-    all = wg_sum(all, sh.red);
+    __syncthreads();
+    const u64 all = wg_sum(sh.tsum[2 * tid] + sh.tsum[2 * tid + 1], sh.red);
+    if (!open) {
+      mass = (double)all * 0x1p-44;
+      step = mass_left ? kMass : kDraw;
+      continue;
+    }
+    mass_left = false;
     const int nb = sh.out32[1];
-    if (nb > kCap) continue;
-    last_listed(sh, nb, want_mass, true, all, tau, tau_idx, weight44);
+    goal = (u64)ceil(want * 0x1p44);
+    if (nb < 1 || nb > kCap) {
+      step = kBits;
+      continue;
+    }
+    last_listed(sh, nb, goal, true, all, tau, tau_idx, weight44);
     for (int i = tid; i < nb; i += kThreads) {
       const u64 x = sh.list[i];
       const int j = (int)(uint32_t)x;
       const double w = weight(list_logit(x));
       if (kept(list_logit(x), j) && w >= mind) atomicAdd(&sh.tsum[j / kTile], fixed44(w));
     }
-    break;
+    step = kDraw;
   }
+
+  // the tile in which the running sum passes u * total, and the token
   __syncthreads();
-  const u64 s0 = sh.tsum[2 * tid], s1 = sh.tsum[2 * tid + 1];
-  u64 total;
-  const u64 base = wg_scan(s0 + s1, sh.red, total);
-  const u64 t = (u64)((double)s.u * (double)total);
-  if (base <= t && t < base + s0 + s1) {
-    const bool second = t >= base + s0;
-    sh.out32[0] = 2 * tid + second;
-    sh.out64[0] = base + (second ? s0 : 0);
+  double m0 = 0.0, m1 = 0.0, total;
+  if (whole) {
+    if (2 * tid < a.ntile) m0 = sh.tmass[2 * tid];
+    if (2 * tid + 1 < a.ntile) m1 = sh.tmass[2 * tid + 1];
+  } else {
+    m0 = (double)sh.tsum[2 * tid] * 0x1p-44;
+    m1 = (double)sh.tsum[2 * tid + 1] * 0x1p-44;
   }
+  const double base = wg_scan(m0 + m1, sh.red, total), t = (double)s.u * total;
+  int tile = wg_min(base + m0 > t && m0 > 0.0 ? 2 * tid : base + (m0 + m1) > t && m1 > 0.0 ? 2 * tid + 1 : INT_MAX, sh.red);
+  if (tile == INT_MAX)  // rounding: the last tile with any weight
+    tile = -wg_min(m1 > 0.0 ? -(2 * tid + 1) : m0 > 0.0 ? -2 * tid : INT_MAX, sh.red);
+  if (tid == tile / 2) sh.out64[0] = __double_as_longlong(base + (tile & 1 ? m0 : 0.0));
   __syncthreads();
   if (wave == 0) {
-    const int j = sh.out32[0] * kTile + 4 * lane;
-    const f32x4 l = tile_quad(a, row, sh.out32[0]);
-    u64 w[4], ls = 0;
+    const f32x4 l = tile_quad(a, row, tile);
+    const int j = tile * kTile + 4 * lane;
+    double w[4], ls = 0.0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      w[e] = 0;
-      if (kept(l[e], j + e)) {
-        const double x = weight(l[e]);
-        if (x >= mind) w[e] = fixed44(x);
-      }
+      w[e] = kept(l[e], j + e) ? weight(l[e]) : 0.0;
+      if (!(w[e] >= mind)) w[e] = 0.0;
       ls += w[e];
     }
-    u64 run = sh.out64[0] + wave_scan(ls) - ls;
+    double run = __longlong_as_double(sh.out64[0]) + (wave_scan(ls) - ls);
+    int at = INT_MAX, last = -1;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      if (run <= t && t < run + w[e]) sh.out32[2] = j + e;
       run += w[e];
+      if (w[e] > 0.0) {
+        if (run > t && at == INT_MAX) at = j + e;
+        last = j + e;
+      }
+    }
+    for (int o = 32; o > 0; o >>= 1) {
+      at = min(at, __shfl_xor(at, o));
+      last = max(last, __shfl_xor(last, o));
+    }
+    if (lane == 0) {
+      a.tokens[r] = at == INT_MAX ? last : at;
+      a.head[r] = {1.0 / total, m, tau, tau_idx};
     }
   }
-  __syncthreads();
-  done(sh.out32[2], tau, tau_idx, (double)total * 0x1p-44);
 }
 
 // The distribution.  grid (rows, ceil(ntile / kTilesPerWg)).
