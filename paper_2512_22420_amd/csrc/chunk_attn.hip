@@ -280,18 +280,20 @@ __device__ __forceinline__ float page_at(const void* p, size_t i) {
   if constexpr (PT == kPageE4M3) return __builtin_amdgcn_cvt_f32_fp8((int)static_cast<const uint8_t*>(p)[i], 0);
 }
 
-// One query row over keys k0 .. k1-1 by a workgroup of 256, 256 keys at a time: a
-// thread scores one key, then sums output dims t and t + 256 (any head dim up to
-// 512).  Only keys in the range are touched.  m in the log2 domain; o unnormalised.
+// One query row over keys k0 .. k1-1 by a workgroup of 256, 256 keys at a time (any head
+// dim up to 512, D % 8 == 0): a thread scores one key, then sums dims t % D and t + 256
+// of the 16-key blocks t / D, t / D + 256 / D, ..: a dim's 16 keys of a block lie side
+// by side.  Keys outside the range count for nothing, whatever they hold.  m in the log2
+// domain; o unnormalised.
 constexpr int kMaxD = 512;
 struct RowLds {
-  float q[kMaxD], p[256], red[4];
+  float q[kMaxD], p[256], o[256], red[4];
   int id[16];
 };
 template <int PT, typename T>
 __device__ void attend_row(const ChunkAttnK& a, int b, int g, const T* q, int k0, int k1, RowLds& sh, float& m, float& l,
                            float (&o)[2]) {
-  const int t = threadIdx.x, D = a.D;
+  const int t = threadIdx.x, D = a.D, groups = max(1, 256 / D);
   __syncthreads();
   for (int d = t; d < D; d += 256) sh.q[d] = to_f(q[d]);
   m = -INFINITY;
@@ -313,8 +315,12 @@ __device__ void attend_row(const ChunkAttnK& a, int b, int g, const T* q, int k0
     float sc = -INFINITY;
     if (k < k1 && id >= 0) {
       const size_t slot = ((size_t)id * a.Hkv + g) * kBlock + t % kBlock;
-      float dot = 0.f;
-      for (int d = 0; d < D; ++d) dot = fmaf(sh.q[d], page_at<PT>(a.kp, slot * D + d), dot);
+      float dots[8] = {};
+#pragma unroll 4
+      for (int d = 0; d < D; d += 8)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dots[e] = fmaf(sh.q[d + e], page_at<PT>(a.kp, slot * D + d + e), dots[e]);
+      float dot = ((dots[0] + dots[1]) + (dots[2] + dots[3])) + ((dots[4] + dots[5]) + (dots[6] + dots[7]));
       if constexpr (PT == kPageE4M3) dot *= __uint_as_float((uint32_t)a.ks[slot] << 23);
       sc = dot * a.scale_log2;
     }
@@ -325,20 +331,32 @@ __device__ void attend_row(const ChunkAttnK& a, int b, int g, const T* q, int k0
     l = l * al + block_sum<256>(p, sh.red);
     sh.p[t] = p;
     __syncthreads();
+    const int nblk = (min(k1 - b0, 256) + kBlock - 1) / kBlock;
     for (int e = 0; e < 2; ++e) {
-      const int d = t + 256 * e;
-      if (d >= D) break;
+      const int d = D < 256 ? t % D : t + 256 * e;
+      if (d >= D || (e && D < 256)) break;
       float acc = o[e] * al;
-      for (int j = 0; j < 256 && b0 + j < k1; ++j) {
-        const int jd = sh.id[j / kBlock];
+      for (int jb = D < 256 ? t / D : 0; jb < nblk && t < groups * D; jb += groups) {
+        const int jd = sh.id[jb], nj = k1 - (b0 + jb * kBlock);
         if (jd < 0) continue;
         const size_t head = ((size_t)jd * a.Hkv + g) * kBlock;
-        float v = page_at<PT>(a.vp, head * D + (size_t)d * kBlock + j % kBlock);
-        if constexpr (PT == kPageE4M3) v *= __uint_as_float((uint32_t)a.vs[head + j % kBlock] << 23);
-        acc = fmaf(sh.p[j], v, acc);
+        float v[kBlock];
+#pragma unroll
+        for (int j = 0; j < kBlock; ++j) v[j] = page_at<PT>(a.vp, head * D + (size_t)d * kBlock + j);
+#pragma unroll
+        for (int j = 0; j < kBlock; ++j) {
+          if constexpr (PT == kPageE4M3) v[j] *= __uint_as_float((uint32_t)a.vs[head + j] << 23);
+          if (j < nj) acc = fmaf(sh.p[jb * kBlock + j], v[j], acc);
+        }
       }
       o[e] = acc;
     }
+  }
+  if (groups > 1) {  // the groups' sums, in order
+    sh.o[t] = o[0];
+    __syncthreads();
+    o[0] = 0.f;
+    for (int q = 0; q < groups && t < D; ++q) o[0] += sh.o[q * D + t];
   }
   if (bad) flag_error(a.c.err, kErrBlock);
 }

@@ -201,15 +201,17 @@ __device__ __forceinline__ u32x4 e4m3_to_bf16x8(u32x2 c, const float (&sc)[8]) {
   return o;
 }
 
-// grid (chunk_units, Hkv): one page block of one sequence and head.  K rows are
-// contiguous; V is turned to rows through LDS.
+// grid (chunk_units, ceil(Hkv / NH)): one page block of one sequence, NH heads, whose
+// loads are all in flight together.  K rows are contiguous; V is turned to rows through
+// LDS.
+constexpr int kLoadMany = 512;  // workgroups
 constexpr int kLoadRow = kD + 8;  // LDS row stride in elements
-template <int PT>
+template <int PT, int NH>
 __global__ __launch_bounds__(256) void chunk_load_kernel(ChunkK a, int Hkv, const void* __restrict__ kp,
                                                          const void* __restrict__ vp, const uint8_t* __restrict__ ks,
                                                          const uint8_t* __restrict__ vs, bf16_t* __restrict__ k_out,
                                                          bf16_t* __restrict__ v_out) {
-  __shared__ __attribute__((aligned(16))) bf16_t s_v[kBlock][kLoadRow];
+  __shared__ __attribute__((aligned(16))) bf16_t s_v[NH][kBlock][kLoadRow];
   if (blockIdx.x == 0 && blockIdx.y == 0) chunk_check(a);
   const ChunkUnit u = chunk_unit(a, blockIdx.x);
   if (u.nt == 0) return;
@@ -217,37 +219,56 @@ __global__ __launch_bounds__(256) void chunk_load_kernel(ChunkK a, int Hkv, cons
     if (blockIdx.y == 0 && threadIdx.x == 0) flag_error(a.err, kErrBlock);
     return;
   }
-  const int g = blockIdx.y, t = threadIdx.x;
-  const size_t head = ((size_t)u.phys * Hkv + g) * kBlock;
+  const int g0 = blockIdx.y * NH, t = threadIdx.x;
   const int tok = t >> 4, e0 = 8 * (t & 15);  // K: this thread's row and dims
   const int d = t >> 1, t0 = 8 * (t & 1);     // V: this thread's dim and slots
   const int i = tok - u.slot0;
   const bool on = i >= 0 && i < u.nt;
-  u32x4 kx, vx;
+  u32x4 kx[NH], vx[NH];
   if constexpr (PT == kPageE4M3) {
-    const u32x2 kc = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(kp) + (head + tok) * kD + e0);
-    const u32x2 vc = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(vp) + head * kD + d * kBlock + t0);
-    const u32x2 vb = *reinterpret_cast<const u32x2*>(vs + head + t0);
-    const float kscale = __uint_as_float((uint32_t)ks[head + tok] << 23);
-    float sk[8], sv[8];
+    u32x2 kc[NH], vc[NH], vb[NH];
+    uint8_t kb[NH];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      sk[e] = kscale;
-      sv[e] = __uint_as_float(((vb[e >> 2] >> (8 * (e & 3))) & 0xffu) << 23);
+    for (int q = 0; q < NH; ++q) {
+      const size_t head = ((size_t)u.phys * Hkv + min(g0 + q, Hkv - 1)) * kBlock;
+      kc[q] = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(kp) + (head + tok) * kD + e0);
+      vc[q] = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(vp) + head * kD + d * kBlock + t0);
+      vb[q] = *reinterpret_cast<const u32x2*>(vs + head + t0);
+      kb[q] = ks[head + tok];
     }
-    kx = e4m3_to_bf16x8(kc, sk);
-    vx = e4m3_to_bf16x8(vc, sv);
+#pragma unroll
+    for (int q = 0; q < NH; ++q) {
+      const float kscale = __uint_as_float((uint32_t)kb[q] << 23);
+      float sk[8], sv[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        sk[e] = kscale;
+        sv[e] = __uint_as_float(((vb[q][e >> 2] >> (8 * (e & 3))) & 0xffu) << 23);
+      }
+      kx[q] = e4m3_to_bf16x8(kc[q], sk);
+      vx[q] = e4m3_to_bf16x8(vc[q], sv);
+    }
   } else {
-    kx = *reinterpret_cast<const u32x4*>(static_cast<const bf16_t*>(kp) + (head + tok) * kD + e0);
-    vx = *reinterpret_cast<const u32x4*>(static_cast<const bf16_t*>(vp) + head * kD + d * kBlock + t0);
+#pragma unroll
+    for (int q = 0; q < NH; ++q) {
+      const size_t head = ((size_t)u.phys * Hkv + min(g0 + q, Hkv - 1)) * kBlock;
+      kx[q] = *reinterpret_cast<const u32x4*>(static_cast<const bf16_t*>(kp) + (head + tok) * kD + e0);
+      vx[q] = *reinterpret_cast<const u32x4*>(static_cast<const bf16_t*>(vp) + head * kD + d * kBlock + t0);
+    }
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) s_v[t0 + e][d] = (bf16_t)(vx[e >> 1] >> (16 * (e & 1)));
+  for (int q = 0; q < NH; ++q)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s_v[q][t0 + e][d] = (bf16_t)(vx[q][e >> 1] >> (16 * (e & 1)));
   __syncthreads();
   if (!on) return;
-  const size_t at = ((size_t)(u.row0 + i) * Hkv + g) * kD + e0;
-  *reinterpret_cast<u32x4*>(k_out + at) = kx;
-  *reinterpret_cast<u32x4*>(v_out + at) = *reinterpret_cast<const u32x4*>(&s_v[tok][e0]);
+#pragma unroll
+  for (int q = 0; q < NH; ++q) {
+    if (g0 + q >= Hkv) break;
+    const size_t at = ((size_t)(u.row0 + i) * Hkv + g0 + q) * kD + e0;
+    *reinterpret_cast<u32x4*>(k_out + at) = kx[q];
+    *reinterpret_cast<u32x4*>(v_out + at) = *reinterpret_cast<const u32x4*>(&s_v[q][tok][e0]);
+  }
 }
 
 // The fp32 path: one thread per (row, KV head, dim).  grid (rows, pieces of Hkv * D).
@@ -301,8 +322,12 @@ hipError_t launch_chunk_load(const ChunkK& a, int pages, int Hkv, int D, const v
                        static_cast<float*>(v_out));
     return hipGetLastError();
   }
-  auto kern = pages == kPageE4M3 ? chunk_load_kernel<kPageE4M3> : chunk_load_kernel<kPageBF16>;
-  hipLaunchKernelGGL(kern, dim3(chunk_units(a.B, a.rows), Hkv), dim3(256), 0, s, a, Hkv, k, v,
+  // Four heads a workgroup where that leaves two a CU (32 contexts of 1500, 7B layout, e4m3: 35 us, 4.2 TB/s, one
+  // head a workgroup 44; a context of 8000, 8B layout: 10.7 and 11.7), else one (a context of 2000: 5.2 us, four 5.6).
+  const int units = chunk_units(a.B, a.rows), nh = units * ((Hkv + 3) / 4) >= kLoadMany ? 4 : 1;
+  auto kern = nh == 4 ? (pages == kPageE4M3 ? chunk_load_kernel<kPageE4M3, 4> : chunk_load_kernel<kPageBF16, 4>)
+                      : (pages == kPageE4M3 ? chunk_load_kernel<kPageE4M3, 1> : chunk_load_kernel<kPageBF16, 1>);
+  hipLaunchKernelGGL(kern, dim3(units, (Hkv + nh - 1) / nh), dim3(256), 0, s, a, Hkv, k, v,
                      static_cast<const uint8_t*>(ks), static_cast<const uint8_t*>(vs), static_cast<bf16_t*>(k_out),
                      static_cast<bf16_t*>(v_out));
   return hipGetLastError();
