@@ -120,15 +120,31 @@ __device__ __forceinline__ RowSet row_set(const SampleK& a, int r) {
   return s;
 }
 
-// Four tokens of a lane: tile t's tokens 4 lane ..; past the end -inf.
-__device__ __forceinline__ f32x4 tile_quad(const SampleK& a, const float* __restrict__ row, int t) {
-  const int j = t * kTile + 4 * (int)(threadIdx.x & 63);
-  if (a.vec && j + 3 < a.V) return *reinterpret_cast<const f32x4*>(row + j);
-  f32x4 l;
+// Four tokens of a lane in each of the wave's N tiles (the same in all lanes): tile
+// t[i]'s tokens 4 lane ..; past the end -inf.  Whole tiles are loaded without conditions,
+// so that all loads are in flight together.
+template <int N>
+__device__ __forceinline__ void tile_quads(const SampleK& a, const float* __restrict__ row, const int (&t)[N], f32x4 (&l)[N]) {
+  const int j = 4 * (int)(threadIdx.x & 63);
+  bool whole = a.vec;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) l[e] = j + e < a.V ? row[j + e] : -INFINITY;
-  return l;
+  for (int i = 0; i < N; ++i) whole &= (t[i] + 1) * kTile <= a.V;
+  if (whole) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) l[i] = *reinterpret_cast<const f32x4*>(row + t[i] * kTile + j);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) l[i][e] = t[i] * kTile + j + e < a.V ? row[t[i] * kTile + j + e] : -INFINITY;
+  }
 }
+__device__ __forceinline__ f32x4 tile_quad(const SampleK& a, const float* __restrict__ row, int t) {
+  f32x4 l[1];
+  tile_quads<1>(a, row, {__builtin_amdgcn_readfirstlane(t)}, l);
+  return l[0];
+}
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
 // Running sums over a wave (inclusive) in a fixed order, each step one move between
 // lanes in registers; lane 63 ends with the wave's.
@@ -183,12 +199,10 @@ __device__ __forceinline__ float wave_max(float v) {
 // grid (rows, ceil(ntile / kTilesPerWg)); a wave reads its four tiles at once.
 constexpr int kWaveTiles = 4, kTilesPerWg = 4 * kWaveTiles;
 __global__ __launch_bounds__(256) void sample_tiles_kernel(SampleK a) {
-  const int r = blockIdx.x, lane = threadIdx.x & 63, t0 = blockIdx.y * kTilesPerWg + (threadIdx.x >> 6) * kWaveTiles;
+  const int r = blockIdx.x, lane = threadIdx.x & 63, t0 = blockIdx.y * kTilesPerWg + wave_id() * kWaveTiles;
   const float* row = a.logits + (size_t)r * a.lstride;
   f32x4 l[kWaveTiles];
-#pragma unroll
-  for (int i = 0; i < kWaveTiles; ++i)
-    if (t0 + i < a.ntile) l[i] = tile_quad(a, row, t0 + i);
+  tile_quads<kWaveTiles>(a, row, {t0, t0 + 1, t0 + 2, t0 + 3}, l);
   const RowSet s = row_set(a, r);
 #pragma unroll
   for (int i = 0; i < kWaveTiles; ++i) {
@@ -263,33 +277,41 @@ __device__ __forceinline__ int wg_min(int v, void* scratch) {
 }
 
 // f(round, j, l[4]) for every four tokens j .. j+3 of the row, thread t of each round
-// the four at round * 4096 + 4 t; tokens past the end are -inf.  Four rounds' loads are
-// in flight while the four before are worked on.
+// the four at round * 4096 + 4 t; tokens past the end are -inf.  While four whole rounds
+// are worked on, the next four are loaded, without conditions: a load under one is
+// waited for before its register's other value can be written.
 template <typename F>
 __device__ __forceinline__ void each4(const SampleK& a, const float* __restrict__ row, F f) {
   constexpr int NR = 4;
-  const int rounds = (a.V + 4 * kThreads - 1) / (4 * kThreads);
-  auto load = [&](int r) {
-    const int j = (r * kThreads + (int)threadIdx.x) * 4;
-    if (a.vec && j + 3 < a.V) return *reinterpret_cast<const f32x4*>(row + j);
+  const int whole = a.vec ? a.V / (4 * kThreads) / NR * NR : 0, t4 = 4 * (int)threadIdx.x;
+  if (whole) {
+    const f32x4* src = reinterpret_cast<const f32x4*>(row) + threadIdx.x;
+    f32x4 next[NR];
+#pragma unroll
+    for (int i = 0; i < NR; ++i) next[i] = src[i * kThreads];
+#pragma unroll 1
+    for (int r = 0; r < whole; r += NR) {
+      f32x4 l[NR];
+      const int ahead = min(r + NR, whole - NR);
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
+        l[i] = next[i];
+        next[i] = src[(ahead + i) * kThreads];
+      }
+#pragma unroll
+      for (int i = 0; i < NR; ++i) f(r + i, (r + i) * 4 * kThreads + t4, l[i]);
+    }
+  }
+#pragma unroll 1
+  for (int r = whole; r * 4 * kThreads < a.V; ++r) {
+    const int j = r * 4 * kThreads + t4;
     f32x4 l;
+    if (a.vec && j + 3 < a.V)
+      l = *reinterpret_cast<const f32x4*>(row + j);
+    else
 #pragma unroll
-    for (int e = 0; e < 4; ++e) l[e] = j + e < a.V ? row[j + e] : -INFINITY;
-    return l;
-  };
-  f32x4 next[NR];
-#pragma unroll
-  for (int i = 0; i < NR; ++i) next[i] = load(i);
-  for (int r = 0; r < rounds; r += NR) {
-    f32x4 l[NR];
-#pragma unroll
-    for (int i = 0; i < NR; ++i) l[i] = next[i];
-    if (r + NR < rounds)
-#pragma unroll
-      for (int i = 0; i < NR; ++i) next[i] = load(r + NR + i);
-#pragma unroll
-    for (int i = 0; i < NR; ++i)
-      if (r + i < rounds) f(r + i, ((r + i) * kThreads + (int)threadIdx.x) * 4, l[i]);
+      for (int e = 0; e < 4; ++e) l[e] = j + e < a.V ? row[j + e] : -INFINITY;
+    f(r, j, l);
   }
 }
 
@@ -479,24 +501,22 @@ __device__ __forceinline__ int nth_equal(const SampleK& a, const float* row, Sha
 // is read, and kCap + 1 returned.
 template <typename F>
 __device__ __forceinline__ int collect(const SampleK& a, const float* row, Shared& sh, float cut, bool guess, F in) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
   __syncthreads();
   if (tid < 2) sh.out32[tid] = 0;
   __syncthreads();
   for (int t = tid; t < a.ntile; t += kThreads)
     if (sh.tmax[t] >= cut && sh.tmax[t] > -INFINITY) sh.tiles[atomicAdd(&sh.out32[0], 1)] = (uint16_t)t;
   __syncthreads();
-  const int nq = sh.out32[0];
+  const int nq = __builtin_amdgcn_readfirstlane(sh.out32[0]);
   if (guess && nq > (1.f - __expf(-(float)kCap / a.ntile)) * a.ntile + 0.5f) return kCap + 1;
   constexpr int NI = 4;  // tiles in flight per wave
   for (int i = wave; i < nq; i += NI * kWaves) {
     f32x4 l[NI];
     int t[NI];
 #pragma unroll
-    for (int q = 0; q < NI; ++q) {
-      t[q] = sh.tiles[min(i + q * kWaves, nq - 1)];
-      l[q] = tile_quad(a, row, t[q]);
-    }
+    for (int q = 0; q < NI; ++q) t[q] = __builtin_amdgcn_readfirstlane(sh.tiles[min(i + q * kWaves, nq - 1)]);
+    tile_quads<NI>(a, row, t, l);
 #pragma unroll
     for (int q = 0; q < NI; ++q) {
       if (i + q * kWaves >= nq) break;  // uniform
@@ -670,6 +690,12 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
     } else {
       cut = !s.by_mass ? (float)(md + (log2(mind) - 1e-6) / s.scale) : round < kGuesses ? (float)(md + kGuess[round] / s.scale) : -INFINITY;
       cut = fminf(cut, m) - fabsf(cut) * 0x1p-22f;
+      if (s.by_mass && cut > -INFINITY) {  // do the tiles with tokens above it hold enough at all?
+        double most = 0.0;
+        for (int t = tid; t < a.ntile; t += kThreads)
+          if (sh.tmax[t] >= cut) most += sh.tmass[t];
+        if (wg_sum(most, sh.red) < (double)s.P * mass) continue;
+      }
     }
     n = collect(a, row, sh, cut, !s.by_count, [&](float l) { return l >= cut; });
     if (n > kCap) break;
@@ -881,7 +907,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
 
 // The distribution.  grid (rows, ceil(ntile / kTilesPerWg)).
 __global__ __launch_bounds__(256) void sample_probs_kernel(SampleK a) {
-  const int r = blockIdx.x, lane = threadIdx.x & 63, t0 = blockIdx.y * kTilesPerWg + (threadIdx.x >> 6) * kWaveTiles;
+  const int r = blockIdx.x, lane = threadIdx.x & 63, t0 = blockIdx.y * kTilesPerWg + wave_id() * kWaveTiles;
   const float* row = a.logits + (size_t)r * a.lstride;
   float* out = a.probs + (size_t)r * a.pstride;
   const RowHead h = a.head[r];
@@ -890,13 +916,12 @@ __global__ __launch_bounds__(256) void sample_probs_kernel(SampleK a) {
   bool any[kWaveTiles];
 #pragma unroll
   for (int i = 0; i < kWaveTiles; ++i) {
-    any[i] = false;
-    if (t0 + i < a.ntile) {
-      const float m = a.tmax[(size_t)r * a.ntile + t0 + i];
-      any[i] = h.inv > 0.0 && m >= h.tau && m > -INFINITY;
-      if (any[i]) l[i] = tile_quad(a, row, t0 + i);
-    }
+    const float m = a.tmax[(size_t)r * a.ntile + min(t0 + i, a.ntile - 1)];
+    any[i] = h.inv > 0.0 && m >= h.tau && m > -INFINITY;
   }
+#pragma unroll
+  for (int i = 0; i < kWaveTiles; ++i)
+    if (t0 + i < a.ntile && any[i]) l[i] = tile_quad(a, row, t0 + i);
 #pragma unroll
   for (int i = 0; i < kWaveTiles; ++i) {
     if (t0 + i >= a.ntile) break;
