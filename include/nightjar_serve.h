@@ -71,7 +71,8 @@ typedef struct nj_kv_layer {
  *   max_chunk     no sequence has more new tokens than this (1 <= max_chunk <= rows)
  *
  * A sequence that breaks these rules, or whose positions do not fit the block
- * table, is skipped whole (NJ_DEV_BAD_CONTEXT); a token whose block id is
+ * table, is skipped whole (NJ_DEV_BAD_CONTEXT; where starts decrease, rows of other
+ * sequences may be skipped with it); a token whose block id is
  * outside [0, num_blocks) is skipped (NJ_DEV_BAD_BLOCK; an attention row that
  * needs such a block is undefined).
  */
@@ -102,7 +103,8 @@ size_t nightjar_chunk_attn_workspace_bytes(const nj_model_desc* desc, int32_t B,
  *   qkv         device fp32, row r at qkv + r * qkv_stride: [q | k | v] of
  *               (H + 2 Hkv) * D values, as the QKV projection gives them
  *               (nightjar_gemm); 16-byte aligned, qkv_stride % 4 == 0
- *   q_out       device [rows][H][D] (desc dtype), 16-byte aligned: rotated queries; NULL: not wanted
+ *   q_out       device [rows][H][D] (desc dtype), 16-byte aligned: rotated queries, apart from qkv;
+ *               NULL: not wanted
  * Rotation as in nightjar_rmsnorm_rope (rotate-half, pair (j, j + D/2) turns by
  * position * rope_theta^(-2j/D)), angle and products in 64 bits, rounded once.
  * NJ_E4M3: a head row's scale is the smallest power of two 2^e with
@@ -119,7 +121,8 @@ int nightjar_chunk_store(const nj_model_desc* desc, const nj_kv_layer* kv, const
 
 /*
  * nightjar_chunk_load -- reads the chunk's positions back from the pages:
- *   k_out, v_out   device [rows][Hkv][D] (desc dtype), 16-byte aligned; 8-bit values are exact in bf16
+ *   k_out, v_out   device [rows][Hkv][D] (desc dtype), 16-byte aligned, apart from each other;
+ *                  8-bit values are exact in bf16
  * With context_lens 0 and n_b the cached lengths it reads whole contexts.
  */
 int nightjar_chunk_load(const nj_model_desc* desc, const nj_kv_layer* kv, const nj_chunk_batch* batch, void* k_out,

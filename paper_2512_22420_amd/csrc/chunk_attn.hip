@@ -371,7 +371,7 @@ __global__ __launch_bounds__(256) void chunk_attn_row_kernel(ChunkAttnK a) {
   if (b < 0) return;
   const ChunkSeq s = chunk_seq(a.c, b);
   const int i = row - s.s0;
-  if (i >= s.n) return;
+  if (i < 0 || i >= s.n) return;  // (before it: where starts decrease)
   float m, l, o[2];
   const size_t at = ((size_t)row * a.H + h) * D;
   attend_row<PT, T>(a, b, h / (a.H / a.Hkv), static_cast<const T*>(a.q) + at, 0, s.c + i + 1, sh, m, l, o);
@@ -1148,6 +1148,9 @@ bool batch_sizes(const char* what, int32_t B, int32_t rows, int32_t max_chunk) {
   return true;
 }
 
+bool overlap(const void* a, size_t an, const void* b, size_t bn) {
+  return (uintptr_t)a < (uintptr_t)b + bn && (uintptr_t)b < (uintptr_t)a + an;
+}
 bool al16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
 // The checks that the chunk calls share; fills the kernels' view of the batch.
@@ -1264,6 +1267,9 @@ int nightjar_chunk_store(const nj_model_desc* desc, const nj_kv_layer* kv, const
   if (qkv_stride < (int64_t)(d.n_heads + 2 * d.n_kv_heads) * d.head_dim || qkv_stride % 4)
     return set_last_error(NJ_EINVAL, "chunk_store: qkv_stride must be a multiple of 4, at least (H + 2 Hkv) * D");
   if (!al16(qkv) || !al16(q_out)) return set_last_error(NJ_EINVAL, "chunk_store: qkv and q_out must be 16-byte aligned");
+  const size_t in_bytes = ((size_t)(batch->rows - 1) * qkv_stride + (d.n_heads + 2 * d.n_kv_heads) * d.head_dim) * 4;
+  if (q_out && overlap(qkv, in_bytes, q_out, (size_t)batch->rows * d.n_heads * d.head_dim * (d.dtype == NJ_F32 ? 4 : 2)))
+    return set_last_error(NJ_EINVAL, "chunk_store: qkv and q_out overlap");
   const hipError_t e = launch_chunk_store(a, page_type(kv), qkv, qkv_stride, d.n_heads, d.n_kv_heads, d.head_dim,
                                           d.rope_theta, q_out, kv->k, kv->v, kv->k_scale, kv->v_scale, (hipStream_t)stream);
   return e == hipSuccess ? NJ_OK : set_last_error(NJ_EHIP, "chunk_store: %s", hipGetErrorString(e));
@@ -1277,6 +1283,8 @@ int nightjar_chunk_load(const nj_model_desc* desc, const nj_kv_layer* kv, const 
     return NJ_EINVAL;
   if (!k_out || !v_out || !al16(k_out) || !al16(v_out))
     return set_last_error(NJ_EINVAL, "chunk_load: k_out and v_out must be 16-byte aligned and not NULL");
+  const size_t out_bytes = (size_t)batch->rows * desc->n_kv_heads * desc->head_dim * (desc->dtype == NJ_F32 ? 4 : 2);
+  if (overlap(k_out, out_bytes, v_out, out_bytes)) return set_last_error(NJ_EINVAL, "chunk_load: k_out and v_out overlap");
   const hipError_t e = launch_chunk_load(a, page_type(kv), desc->n_kv_heads, desc->head_dim, kv->k, kv->v, kv->k_scale,
                                          kv->v_scale, k_out, v_out, (hipStream_t)stream);
   return e == hipSuccess ? NJ_OK : set_last_error(NJ_EHIP, "chunk_load: %s", hipGetErrorString(e));
@@ -1298,7 +1306,7 @@ int nightjar_chunk_attn(const nj_model_desc* desc, const nj_kv_layer* kv, const 
     return set_last_error(NJ_EINVAL, "chunk_attn: q and out must be 16-byte aligned and not NULL");
   const nj_model_desc& d = *desc;
   const size_t row_bytes = (size_t)batch->rows * d.n_heads * d.head_dim * (d.dtype == NJ_F32 ? 4 : 2);
-  if ((uintptr_t)q < (uintptr_t)out + row_bytes && (uintptr_t)out < (uintptr_t)q + row_bytes)
+  if (overlap(q, row_bytes, out, row_bytes))
     return set_last_error(NJ_EINVAL, "chunk_attn: q and out overlap");
   const AttnParts p = attn_parts(d, batch->max_chunk);
   ChunkAttnK a{};

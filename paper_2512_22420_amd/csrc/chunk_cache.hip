@@ -154,7 +154,7 @@ __global__ __launch_bounds__(256) void chunk_store_f32_kernel(ChunkK a, const fl
   if (b < 0) return;
   const ChunkSeq s = chunk_seq(a, b);
   const int i = row - s.s0;
-  if (i >= s.n) return;
+  if (i < 0 || i >= s.n) return;  // (before it: where starts decrease)
   const int half = D / 2, t = blockIdx.y * 256 + threadIdx.x;
   if (t >= (H + 2 * Hkv) * half) return;
   const int hd = t / half, j = t % half, pos = s.c + i;
@@ -281,7 +281,7 @@ __global__ __launch_bounds__(256) void chunk_load_f32_kernel(ChunkK a, int Hkv, 
   if (b < 0) return;
   const ChunkSeq s = chunk_seq(a, b);
   const int i = row - s.s0, t = blockIdx.y * 256 + threadIdx.x;
-  if (i >= s.n || t >= Hkv * D) return;
+  if (i < 0 || i >= s.n || t >= Hkv * D) return;
   const int g = t / D, d = t % D, pos = s.c + i;
   const int id = a.table[(size_t)b * a.max_blocks + pos / kBlock], slot = pos % kBlock;
   if (id < 0 || id >= a.num_blocks) {

@@ -142,6 +142,15 @@ def device_error(ws: Workspace, stream: Optional[int] = None) -> int:
     return nb.device_error(ws.ptr, ws.nbytes, s)
 
 
+def _on_gpu(device: torch.device, *tensors) -> None:
+    """Kernels read these where they are: all on one GPU, the current one."""
+    if device.type != "cuda" or device.index != torch._C._cuda_getDevice():
+        raise TypeError(f"need tensors on the current GPU, got {device}")
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise TypeError(f"need all tensors on {device}, got one on {t.device}")
+
+
 def _current(t: torch.Tensor, stream: Optional[int]) -> int:
     """The stream to enqueue on: the given one, or the current one of the tensor's device (without building a
     torch.cuda.Stream, which takes longer than the rest of a call)."""
@@ -168,6 +177,8 @@ class KvLayer:
             raise TypeError("k_scale and v_scale: needed for e4m3 pages, and for no others")
         for t, n in ((k_scale, "k_scale"), (v_scale, "v_scale")):
             _expect(t, torch.uint8, nb_ * hkv * bs, n)
+        if any(t is not None and t.device != k.device for t in (v, k_scale, v_scale)):
+            raise TypeError("k, v and their scales: need one device")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.hkv, self.head_dim = hkv, D
         self.c = nb.KvLayer(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), nb_, self._DTYPES[k.dtype])
@@ -182,6 +193,8 @@ class ChunkBatch:
         _expect(starts, torch.int32, B + 1, "starts")
         _expect(context_lens, torch.int32, B, "context_lens")
         _expect(block_table, torch.int32, B * block_table.shape[-1], "block_table")
+        if starts.device != context_lens.device or starts.device != block_table.device:
+            raise TypeError("starts, context_lens and block_table: need one device")
         self.starts, self.context_lens, self.block_table = starts, context_lens, block_table
         self.B, self.rows, self.max_chunk = B, rows, max_chunk
         self.c = nb.ChunkBatch(_ptr(starts), _ptr(context_lens), _ptr(block_table), block_table.shape[-1], B, rows,
@@ -227,6 +240,7 @@ def chunk_store(desc, layer: KvLayer, batch: ChunkBatch, qkv: torch.Tensor, ws: 
     if qkv.dtype != torch.float32 or tuple(qkv.shape) != (batch.rows, width) or qkv.stride(1) != 1:
         raise TypeError(f"qkv: need a float32 tensor [{batch.rows}, {width}] with contiguous rows, got {qkv.dtype} {tuple(qkv.shape)}")
     _expect_layer(desc, layer)
+    _on_gpu(qkv.device, q_out, layer.k, batch.starts, ws.buf)
     if q_out is not None:
         _expect_row(q_out, desc, batch.rows * desc.n_heads * desc.head_dim, "q_out")
     s = _current(qkv, stream)
@@ -240,6 +254,7 @@ def chunk_load(desc, layer: KvLayer, batch: ChunkBatch, k_out: torch.Tensor, v_o
     _expect_layer(desc, layer)
     for t, n in ((k_out, "k_out"), (v_out, "v_out")):
         _expect_row(t, desc, batch.rows * desc.n_kv_heads * desc.head_dim, n)
+    _on_gpu(k_out.device, v_out, layer.k, batch.starts, ws.buf)
     s = _current(k_out, stream)
     nb.chunk_load(desc, layer.c, batch.c, k_out.data_ptr(), v_out.data_ptr(), ws.ptr, ws.nbytes, s)
 
@@ -250,6 +265,7 @@ def chunk_attn(desc, layer: KvLayer, batch: ChunkBatch, q: torch.Tensor, out: to
     _expect_layer(desc, layer)
     for t, n in ((q, "q"), (out, "out")):
         _expect_row(t, desc, batch.rows * desc.n_heads * desc.head_dim, n)
+    _on_gpu(q.device, out, layer.k, batch.starts, ws.buf)
     s = _current(q, stream)
     nb.chunk_attn(desc, layer.c, batch.c, q.data_ptr(), out.data_ptr(), ws.ptr, ws.nbytes, s)
 
@@ -269,6 +285,7 @@ def sample(logits: torch.Tensor, uniforms: torch.Tensor, tokens: torch.Tensor, w
         _expect(t, torch.float32, R, n)
     _expect(tokens, torch.int32, R, "tokens")
     _expect(top_k, torch.int32, R, "top_k")
+    _on_gpu(logits.device, uniforms, tokens, temperature, top_k, top_p, min_p, probs, ws.buf)
     s = _current(logits, stream)
     nb.sample(logits.data_ptr(), logits.stride(0) if R > 1 else V, R, V, _ptr(temperature), _ptr(top_k), _ptr(top_p),
               _ptr(min_p), _ptr(uniforms), _ptr(tokens), _ptr(probs), 0 if probs is None else probs.stride(0) if R > 1 else V,

@@ -375,3 +375,47 @@ def test_attention_of_padded_batches(pages, n):
     chunk_attn(c.desc, c.layer, c.batch, q, out, c.ws)
     assert c.error() == 0 and (out[c.starts[-1]:] == -7).all()
     _check_attn(c, q, out, vals)
+
+
+LONG = [([1], [20000]), ([4], [9000]), ([6, 1], [4000, 9000]), ([40], [6000]), ([9, 150], [3000, 700])]
+
+
+@pytest.mark.parametrize("pages,shape", [("e4m3", L8), ("bf16", L7), ("e4m3", MQA)], ids=["e4m3-8b", "bf16-7b", "e4m3-mqa"])
+@pytest.mark.parametrize("n,ctx", LONG, ids=range(len(LONG)))
+def test_attention_of_long_contexts(pages, shape, n, ctx):
+    """Keys cut into many parts: streamed pieces of one and two row tiles, tiles joined by a launch of their own."""
+    c = Case(shape, pages, n, ctx, seed=21 + len(n))
+    vals = c.fill_context()
+    q = torch.as_tensor(c.rng.normal(size=(c.rows, shape.n_heads, shape.head_dim)) * 1.5).to("cuda", c.rdt)
+    out = torch.empty((c.rows, shape.n_heads * shape.head_dim), dtype=c.rdt, device="cuda")
+    for _ in range(3):  # (the workspace as it was left)
+        out.fill_(-7.0)
+        chunk_attn(c.desc, c.layer, c.batch, q, out, c.ws)
+        _check_attn(c, q, out, vals)
+    assert c.error() == 0
+
+
+@pytest.mark.parametrize("starts", [[0, 10, 5, 20], [3, 2, 20, 20], [20, 0, 10, 20], [0, 20, 0, 20]])
+@pytest.mark.parametrize("pages,shape", [("e4m3", MHA), ("bf16", MHA), ("f32", _shape(2, 2, "f32", 64))], ids=["e4m3", "bf16", "f32"])
+def test_starts_that_decrease(pages, shape, starts):
+    """Flagged, and nothing outside the sequences' own blocks and rows is written."""
+    c = Case(shape, pages, [20, 20, 20], [0, 3, 5], tail=0)
+    c.batch = ChunkBatch(_dev(starts), _dev(c.ctx), _dev(c.table), 20, 20)
+    kind = {"e4m3": torch.uint8, "bf16": torch.int16, "f32": torch.int32}[pages]
+    mine = np.zeros((c.pool, 16), bool)
+    for b in range(3):
+        pos = np.arange(c.ctx[b], c.ctx[b] + 20)
+        mine[c.table[b, pos // 16], pos % 16] = True
+    k0, v0 = c.k.clone(), c.v.clone()
+    guard = torch.full((24, 2, shape.head_dim), -7.0, dtype=c.rdt, device="cuda")
+    q = torch.zeros((20, 2, shape.head_dim), dtype=c.rdt, device="cuda")
+    chunk_store(c.desc, c.layer, c.batch, torch.ones((20, 6 * shape.head_dim), device="cuda"), c.ws, q_out=q)
+    assert c.error() == nb.NJ_DEV_BAD_CONTEXT
+    for now, was, at in ((c.k, k0, (0, 2)), (c.v, v0, (0, 3))):
+        d = (now.contiguous().view(kind) != was.contiguous().view(kind)).cpu().numpy()
+        assert not (d.any(axis=tuple(i for i in range(4) if i not in at)) & ~mine).any()
+    out = guard[2:22]
+    chunk_load(c.desc, c.layer, c.batch, q, out, c.ws)
+    assert c.error() == nb.NJ_DEV_BAD_CONTEXT
+    chunk_attn(c.desc, c.layer, c.batch, torch.zeros_like(q), out, c.ws)
+    assert c.error() == nb.NJ_DEV_BAD_CONTEXT and (guard[:2] == -7).all() and (guard[22:] == -7).all()
