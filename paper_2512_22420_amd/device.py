@@ -142,19 +142,14 @@ def device_error(ws: Workspace, stream: Optional[int] = None) -> int:
     return nb.device_error(ws.ptr, ws.nbytes, s)
 
 
-def _on_gpu(device: torch.device, *tensors) -> None:
-    """Kernels read these where they are: all on one GPU, the current one."""
-    if device.type != "cuda" or device.index != torch._C._cuda_getDevice():
-        raise TypeError(f"need tensors on the current GPU, got {device}")
+def _stream_on(stream: Optional[int], *tensors) -> int:
+    """The stream to enqueue on: the given one, or the current one.  The kernels read these tensors where they are: all
+    on the current GPU.  (No torch.device or torch.cuda.Stream is built: either takes longer than the checks.)"""
+    dev = torch._C._cuda_getDevice()
     for t in tensors:
-        if t is not None and t.device != device:
-            raise TypeError(f"need all tensors on {device}, got one on {t.device}")
-
-
-def _current(t: torch.Tensor, stream: Optional[int]) -> int:
-    """The stream to enqueue on: the given one, or the current one of the tensor's device (without building a
-    torch.cuda.Stream, which takes longer than the rest of a call)."""
-    return torch._C._cuda_getCurrentRawStream(t.device.index) if stream is None else stream
+        if t is not None and t.get_device() != dev:
+            raise TypeError(f"need tensors on the current GPU (cuda:{dev}), got one on {t.device}")
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream
 
 
 class KvLayer:
@@ -240,10 +235,9 @@ def chunk_store(desc, layer: KvLayer, batch: ChunkBatch, qkv: torch.Tensor, ws: 
     if qkv.dtype != torch.float32 or tuple(qkv.shape) != (batch.rows, width) or qkv.stride(1) != 1:
         raise TypeError(f"qkv: need a float32 tensor [{batch.rows}, {width}] with contiguous rows, got {qkv.dtype} {tuple(qkv.shape)}")
     _expect_layer(desc, layer)
-    _on_gpu(qkv.device, q_out, layer.k, batch.starts, ws.buf)
     if q_out is not None:
         _expect_row(q_out, desc, batch.rows * desc.n_heads * desc.head_dim, "q_out")
-    s = _current(qkv, stream)
+    s = _stream_on(stream, qkv, q_out, layer.k, batch.starts, ws.buf)
     nb.chunk_store(desc, layer.c, batch.c, qkv.data_ptr(), qkv.stride(0) if batch.rows > 1 else width, _ptr(q_out),
                    ws.ptr, ws.nbytes, s)
 
@@ -254,8 +248,7 @@ def chunk_load(desc, layer: KvLayer, batch: ChunkBatch, k_out: torch.Tensor, v_o
     _expect_layer(desc, layer)
     for t, n in ((k_out, "k_out"), (v_out, "v_out")):
         _expect_row(t, desc, batch.rows * desc.n_kv_heads * desc.head_dim, n)
-    _on_gpu(k_out.device, v_out, layer.k, batch.starts, ws.buf)
-    s = _current(k_out, stream)
+    s = _stream_on(stream, k_out, v_out, layer.k, batch.starts, ws.buf)
     nb.chunk_load(desc, layer.c, batch.c, k_out.data_ptr(), v_out.data_ptr(), ws.ptr, ws.nbytes, s)
 
 
@@ -265,8 +258,7 @@ def chunk_attn(desc, layer: KvLayer, batch: ChunkBatch, q: torch.Tensor, out: to
     _expect_layer(desc, layer)
     for t, n in ((q, "q"), (out, "out")):
         _expect_row(t, desc, batch.rows * desc.n_heads * desc.head_dim, n)
-    _on_gpu(q.device, out, layer.k, batch.starts, ws.buf)
-    s = _current(q, stream)
+    s = _stream_on(stream, q, out, layer.k, batch.starts, ws.buf)
     nb.chunk_attn(desc, layer.c, batch.c, q.data_ptr(), out.data_ptr(), ws.ptr, ws.nbytes, s)
 
 
@@ -285,8 +277,7 @@ def sample(logits: torch.Tensor, uniforms: torch.Tensor, tokens: torch.Tensor, w
         _expect(t, torch.float32, R, n)
     _expect(tokens, torch.int32, R, "tokens")
     _expect(top_k, torch.int32, R, "top_k")
-    _on_gpu(logits.device, uniforms, tokens, temperature, top_k, top_p, min_p, probs, ws.buf)
-    s = _current(logits, stream)
+    s = _stream_on(stream, logits, uniforms, tokens, temperature, top_k, top_p, min_p, probs, ws.buf)
     nb.sample(logits.data_ptr(), logits.stride(0) if R > 1 else V, R, V, _ptr(temperature), _ptr(top_k), _ptr(top_p),
               _ptr(min_p), _ptr(uniforms), _ptr(tokens), _ptr(probs), 0 if probs is None else probs.stride(0) if R > 1 else V,
               ws.ptr, ws.nbytes, s)

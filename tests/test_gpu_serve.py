@@ -347,3 +347,15 @@ def test_two_graphs_on_one_workspace():
             assert torch.equal(c[3], w)
             chunk_attn(desc, c[0], c[1], c[2], c[3], ws)
     assert device_error(ws) == 0
+
+
+def test_tensors_off_the_gpu_are_refused():
+    l, u, t, ws = torch.zeros((2, 8), device="cuda"), torch.zeros(2), torch.zeros(2, dtype=torch.int32, device="cuda"), sample_workspace(2, 8)
+    with pytest.raises(TypeError, match="GPU"):
+        sample(l, u, t, ws)
+    desc, layer = model_desc(F32), _pages(F32, "f32", 2)
+    out = [torch.zeros((3, 4, 64), device=d) for d in ("cuda", "cpu")]
+    for where in ("cuda", "cpu"):
+        batch = ChunkBatch(*(torch.tensor(x, dtype=torch.int32, device=where) for x in ([0, 3], [0], [[0]])), 3, 3)
+        with pytest.raises(TypeError, match="GPU"):
+            chunk_load(desc, layer, batch, out[0], out[int(where == "cuda")], Scratch(256))

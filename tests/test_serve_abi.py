@@ -63,13 +63,6 @@ def test_overlapping_rows_are_refused():
         assert f(c(BF), c(_layer()), c(_batch()), *a, 256, BIG, 0) == nb.NJ_EINVAL and "overlap" in nb.last_error()
 
 
-def test_tensors_off_the_gpu_are_refused():
-    import torch
-    from paper_2512_22420_amd.device import _on_gpu
-    with pytest.raises(TypeError):
-        _on_gpu(torch.zeros(1).device)
-
-
 def test_chunk_calls_refuse_descriptors():
     for field, value in (("n_kv_heads", 5), ("n_kv_heads", 0), ("block_size", 32), ("dtype", 2), ("head_dim", 64),
                          ("head_dim", 12), ("n_heads", 4096)):
