@@ -225,7 +225,7 @@ __global__ __launch_bounds__(256) void sample_tiles_kernel(SampleK a) {
 
 struct Shared {
   union {
-    uint32_t bins[2 * kBins];  // two copies, for even and odd lanes
+    __attribute__((aligned(16))) uint32_t bins[2 * kBins];
     struct {
       u64 mass[kBitBins];
       uint32_t count[kBitBins];
@@ -570,7 +570,53 @@ __device__ __forceinline__ void clear_bins(Shared& sh) {
   for (int i = threadIdx.x; i < kBins / 2; i += kThreads) reinterpret_cast<uint4*>(sh.bins)[i] = uint4{0, 0, 0, 0};
   __syncthreads();
 }
-__device__ __forceinline__ void add_bin(Shared& sh, float d, uint32_t v) { atomicAdd(&sh.bins[d_bin(d) + (threadIdx.x & 1) * kBins], v); }
+__device__ __forceinline__ void add_bin(Shared& sh, int bin, uint32_t v) { atomicAdd(&sh.bins[bin + (threadIdx.x & 1) * kBins], v); }
+
+// The histogram of a row's mass, in units of which it has at most 2^31: a token's weight
+// is computed in fp32 and cut to whole ones, and good for 2^-17.
+__device__ __forceinline__ double mass_unit(double mass) { return 0x1p31 / mass; }
+__device__ __forceinline__ uint32_t mass_units(float d, float scale, float shift) {
+  return (uint32_t)__builtin_amdgcn_exp2f(fmaf(-d, scale, shift));
+}
+// Its bins are even in max - l, `per` to the unit: over 32 bits of weight, or as far as four
+// times the lowest tile's max where that is nearer (a hot or narrow row).
+__device__ __forceinline__ float mass_bins(float lowest, double scale) {
+  return kBins / fmaxf(fminf((float)(32.0 / scale), 4.f * lowest), 0x1p-80f);
+}
+__device__ __forceinline__ int mass_bin(float x) { return (int)fminf(x, kBins - 1.f); }
+// The bracket that it gives of the last token of a prefix of mass `want`: near <= (max - l) * per < far.
+__device__ __forceinline__ void bracket(Shared& sh, const u64 (&x)[5], int V, double want, double unit, float& near, float& far) {
+  const u64 lo = (u64)floor(want * unit), hi = (u64)ceil(want * unit);
+  const int first = first_bin(sh, x, [&](u64 x) { return x + (x >> 16) + V >= lo; });
+  const int last = first_bin(sh, x, [&](u64 x) { return x - (x >> 16) > hi; });
+  near = (float)min(first, kBins - 1);
+  far = last < kBins - 1 ? (float)(last + 1) : INFINITY;
+}
+// The sum of a wave's four tokens a lane that are kept and lie above the bracket, w >= least;
+// `put` takes the kept tokens inside it (open: there is one).
+template <typename K, typename W, typename P>
+__device__ __forceinline__ double sum_above(const f32x4& l, int j, float m, float per, bool open, float near, float far, double least, K kept,
+                                            W weight, P put) {
+  double sum = 0.0;
+  bool any = false;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float x = (m - l[e]) * per;
+    const bool k = kept(l[e], j + e);
+    any |= k && !(x < near) && x < far;
+    const double w = weight(l[e]);
+    // (where w < min_p above the bracket, nothing in it is kept either, so that the sum may lack these)
+    if (k && (!open || x < near) && w >= least) sum += w;
+  }
+  if (open && __any(any)) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float x = (m - l[e]) * per;
+      if (kept(l[e], j + e) && !(x < near) && x < far) put(((u64)~order_key(l[e]) << 32) | (uint32_t)(j + e));
+    }
+  }
+  return wave_scan(sum);
+}
 
 __device__ __forceinline__ float list_logit(u64 v) { return key_logit(~(uint32_t)(v >> 32)); }
 
@@ -672,14 +718,14 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
   // top-p alone: guesses, lowered while the tokens above fall short of the target.
   // min-p alone: its own border (a little below: the test itself decides).
   float cut = -INFINITY;
-  constexpr int kGuesses = 5;
+  constexpr int kGuesses = 5, kManyTiles = 128;
   constexpr float kGuess[kGuesses] = {-5.f, -8.f, -12.f, -16.f, -24.f};  // log2 of the weight
   int n = 0;
   bool listed = false;
   for (int round = 0; !listed && !whole && !(s.by_count && s.K > kCap); ++round) {
     if (s.by_count) {
       clear_bins(sh);
-      for (int t = tid; t < a.ntile; t += kThreads) add_bin(sh, m - sh.tmax[t], 1);
+      for (int t = tid; t < a.ntile; t += kThreads) add_bin(sh, d_bin(m - sh.tmax[t]), 1);
       __syncthreads();
       u64 x[5], all;
       scan_bins(sh, x, all);
@@ -690,10 +736,16 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
     } else {
       cut = !s.by_mass ? (float)(md + (log2(mind) - 1e-6) / s.scale) : round < kGuesses ? (float)(md + kGuess[round] / s.scale) : -INFINITY;
       cut = fminf(cut, m) - fabsf(cut) * 0x1p-22f;
-      if (s.by_mass && cut > -INFINITY) {  // do the tiles with tokens above it hold enough at all?
-        double most = 0.0;
+      if (s.by_mass && cut > -INFINITY && a.ntile > kManyTiles) {
+        // The tokens above it hold no less than their tiles' maxima and no more than these tiles: is that, or (where many
+        // tiles would be read) half way between, enough?
+        double tops = 0.0, most = 0.0;
         for (int t = tid; t < a.ntile; t += kThreads)
-          if (sh.tmax[t] >= cut) most += sh.tmass[t];
+          if (sh.tmax[t] >= cut) {
+            tops += weight(sh.tmax[t]);
+            most += sh.tmass[t];
+          }
+        if (__syncthreads_count(most > 0.0) > kManyTiles) most = 0.5 * (most + tops);
         if (wg_sum(most, sh.red) < (double)s.P * mass) continue;
       }
     }
@@ -755,16 +807,22 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
   enum { kCount, kMass, kBits, kSum, kDraw };
   bool mass_left = s.by_mass;  // top-p is still to do
   u64 goal = 0;                // of the search over the bits
+  float per = 0.f;  // bins per unit of max - l
 #pragma unroll 1
   for (int step = whole || listed ? kDraw : s.by_count ? kCount : s.by_mass ? kMass : kSum; step != kDraw;) {
-    // the mass is at most 2^31 of these units; a token's is cut to whole ones, and good for 2^-17
-    const double unit = 0x1p31 / mass, want = (double)s.P * mass;
-    float near = -1.f, far = INFINITY;  // the bracket: near <= max - l < far
+    const double unit = mass_unit(mass), want = (double)s.P * mass;
+    float near = 0.f, far = INFINITY;
     if (step == kBits) {
       const RadixOut x = radix_search(a, row, sh, s.by_mass && !mass_left, goal, weight44);
       tau = key_logit(x.key);
       tau_idx = nth_equal(a, row, sh, tau, x.need);
       step = kSum;
+    }
+    if (step == kMass) {
+      float lowest = INFINITY;  // tile's max, of those with any token
+      for (int t = tid; t < a.ntile; t += kThreads)
+        if (sh.tmax[t] > -INFINITY) lowest = fminf(lowest, sh.tmax[t]);
+      per = mass_bins(m + wg_max(-lowest, sh.red), s.scale);
     }
     if (step != kSum) {
       clear_bins(sh);
@@ -773,19 +831,16 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           uint32_t u = l[e] > -INFINITY;
-          if (step == kMass) u = kept(l[e], j + e) ? (uint32_t)__builtin_amdgcn_exp2f(fmaf(l[e] - m, scale, shift)) : 0;
-          if (u) add_bin(sh, m - l[e], u);
+          const float d = m - l[e];
+          if (step == kMass) u = kept(l[e], j + e) ? mass_units(d, scale, shift) : 0;
+          if (u) add_bin(sh, step == kMass ? mass_bin(d * per) : d_bin(d), u);
         }
       });
       __syncthreads();
       u64 x[5], all;
       scan_bins(sh, x, all);
       if (step == kMass) {
-        const u64 lo = (u64)floor(want * unit), hi = (u64)ceil(want * unit);
-        const int first = first_bin(sh, x, [&](u64 x) { return x + (x >> 16) + V >= lo; });
-        const int last = first_bin(sh, x, [&](u64 x) { return x - (x >> 16) > hi; });
-        if (first > 0) near = bin_edge(min(first, kBins - 1));
-        if (last < kBins - 1) far = bin_edge(last + 1);
+        bracket(sh, x, V, want, unit, near, far);
       } else {
         const u64 k = min((u64)s.K, all);  // (fewer finite logits than K)
         const int bin = first_bin(sh, x, [&](u64 x) { return x >= k; });
@@ -810,28 +865,10 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
     if (tid == 0) sh.out32[1] = 0;
     __syncthreads();
     each4(a, row, [&](int rd, int j, const f32x4& l) {
-      double sum = 0.0;
-      bool any = false;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float d = m - l[e];
-        const bool k = kept(l[e], j + e);
-        any |= k && !(d < near) && d < far;
-        const double w = weight(l[e]);
-        // (where w < min_p above the bracket, nothing in it is kept either, so that the sum may lack these)
-        if (k && (!open || d < near) && w >= least) sum += w;
-      }
-      if (open && __any(any)) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float d = m - l[e];
-          if (kept(l[e], j + e) && !(d < near) && d < far) {
-            const int at = atomicAdd(&sh.out32[1], 1);
-            if (at < kCap) sh.list[at] = ((u64)~order_key(l[e]) << 32) | (uint32_t)(j + e);
-          }
-        }
-      }
-      sum = wave_scan(sum);
+      const double sum = sum_above(l, j, m, per, open, near, far, least, kept, weight, [&](u64 x) {
+        const int at = atomicAdd(&sh.out32[1], 1);
+        if (at < kCap) sh.list[at] = x;
+      });
       if (lane == 63) sh.tsum[rd * kWaves + wave] = fixed44(sum);
     });
     __syncthreads();

@@ -185,3 +185,23 @@ def test_same_result_whatever_the_batch():
         for r in (0, 4, 8):
             t1, p1, _ = _run(l[r:r + 1], u[r:r + 1], **kw)
             assert t1[0] == tok[r] and np.array_equal(p1[0], probs[r])
+
+
+@pytest.mark.parametrize("kw", [dict(p=0.97), dict(p=0.9, m=0.02), dict(p=0.999, T=1.5), dict(p=0.5, T=3.0), dict(p=0.9, m=0.3)])
+@pytest.mark.parametrize("V,R", [(5003, 33), (50000, 40), (128256, 34)])
+def test_broad_rows_of_large_batches(V, R, kw):
+    """Flat distributions in batches whose long rows are shared between workgroups: flat ones, peaked ones, levels of
+    thousands of equal logits, and rows with a few thousand tokens left; each row the same bits as alone."""
+    rng = np.random.default_rng(V + R)
+    l = rng.standard_normal((R, V)).astype(np.float32)
+    l[1::5] *= 4
+    l[2::5] = np.round(l[2::5])
+    l[3::10] = 0.25
+    l[4, : V // 10] = -np.inf
+    l[9, 4500:] = -np.inf
+    u = rng.random(R).astype(np.float32)
+    _check(l, u, pad=V % 4, **kw)
+    tok, probs, _ = _run(l, u, **kw)
+    for r in (0, 2, 3, 4, 9, 11, 33 % R):
+        t1, p1, _ = _run(l[r:r + 1], u[r:r + 1], **kw)
+        assert t1[0] == tok[r] and np.array_equal(p1[0], probs[r])
