@@ -548,9 +548,10 @@ __device__ __forceinline__ float bin_floor(float m, int b) {
 }
 
 // This thread's four bins, copies joined, as running sums behind what comes before (x[0]).
-__device__ __forceinline__ void scan_bins(Shared& sh, u64 (&x)[5], u64& all) {
+template <typename T>
+__device__ __forceinline__ void scan_bins(Shared& sh, T (&x)[5], T& all) {
   const uint4 a = reinterpret_cast<const uint4*>(sh.bins)[threadIdx.x], b = reinterpret_cast<const uint4*>(sh.bins + kBins)[threadIdx.x];
-  const u64 n[4] = {(u64)a.x + b.x, (u64)a.y + b.y, (u64)a.z + b.z, (u64)a.w + b.w};
+  const T n[4] = {(T)a.x + b.x, (T)a.y + b.y, (T)a.z + b.z, (T)a.w + b.w};
   x[0] = wg_scan(n[0] + n[1] + n[2] + n[3], sh.red, all);
 #pragma unroll
   for (int i = 0; i < 4; ++i) x[i + 1] = x[i] + n[i];
@@ -564,6 +565,14 @@ __device__ __forceinline__ int first_bin(Shared& sh, const u64 (&x)[5], F reache
   for (int i = 3; i >= 0; --i)
     if (reached(x[i + 1])) b = 4 * threadIdx.x + i;
   return wg_min(b, sh.red);
+}
+// The bin in which the running sum comes to k (0 < k <= the sum of all).
+__device__ __forceinline__ int bin_of(Shared& sh, const uint32_t (&x)[5], uint32_t k) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (x[i] < k && k <= x[i + 1]) sh.out32[3] = 4 * threadIdx.x + i;
+  __syncthreads();
+  return sh.out32[3];
 }
 __device__ __forceinline__ void clear_bins(Shared& sh) {
   __syncthreads();
@@ -718,8 +727,8 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
   // top-p alone: guesses, lowered while the tokens above fall short of the target.
   // min-p alone: its own border (a little below: the test itself decides).
   float cut = -INFINITY;
-  constexpr int kGuesses = 5, kManyTiles = 128;
-  constexpr float kGuess[kGuesses] = {-5.f, -8.f, -12.f, -16.f, -24.f};  // log2 of the weight
+  constexpr int kManyTiles = 128;
+  const double bit = s.T * 0.69314718055994530942;  // of weight, in logits
   int n = 0;
   bool listed = false;
   for (int round = 0; !listed && !whole && !(s.by_count && s.K > kCap); ++round) {
@@ -727,14 +736,15 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
       clear_bins(sh);
       for (int t = tid; t < a.ntile; t += kThreads) add_bin(sh, d_bin(m - sh.tmax[t]), 1);
       __syncthreads();
-      u64 x[5], all;
+      uint32_t x[5], all;
       scan_bins(sh, x, all);
       const float aim = (round ? 1.5f : 1.f) * (1.1f * s.K + 4.f * sqrtf((float)s.K));
       const int rank = round >= 2 ? a.ntile : max((int)ceilf((1.f - __expf(-aim / a.ntile)) * a.ntile), 1);
-      const u64 want = min(rank, min(s.K, a.ntile));
-      cut = bin_floor(m, first_bin(sh, x, [&](u64 x) { return x >= want; }));
+      cut = bin_floor(m, bin_of(sh, x, min(rank, min(s.K, a.ntile))));
     } else {
-      cut = !s.by_mass ? (float)(md + (log2(mind) - 1e-6) / s.scale) : round < kGuesses ? (float)(md + kGuess[round] / s.scale) : -INFINITY;
+      // (top-p: 2^-5, -8, -12, -16, -24; selected, as a table would be read from memory)
+      const float guess = round == 0 ? -5.f : round == 1 ? -8.f : round == 2 ? -12.f : round == 3 ? -16.f : -24.f;
+      cut = !s.by_mass ? (float)(md + (log2(mind) - 1e-6) * bit) : round < 5 ? (float)(md + guess * bit) : -INFINITY;
       cut = fminf(cut, m) - fabsf(cut) * 0x1p-22f;
       if (s.by_mass && cut > -INFINITY && a.ntile > kManyTiles) {
         // The tokens above it hold no less than their tiles' maxima and no more than these tiles: is that, or (where many
@@ -791,7 +801,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
       }
       run += w[e];
     }
-    const u64 last = sh.list[wg_sum(cnt, sh.red) - 1];
+    const u64 last = sh.list[(four ? wg_sum(cnt, sh.red) : __syncthreads_count(cnt)) - 1];
     tau = list_logit(last);
     tau_idx = (int)(uint32_t)last;
   }
@@ -837,13 +847,15 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
         }
       });
       __syncthreads();
-      u64 x[5], all;
-      scan_bins(sh, x, all);
       if (step == kMass) {
+        u64 x[5], all;
+        scan_bins(sh, x, all);
         bracket(sh, x, V, want, unit, near, far);
       } else {
-        const u64 k = min((u64)s.K, all);  // (fewer finite logits than K)
-        const int bin = first_bin(sh, x, [&](u64 x) { return x >= k; });
+        uint32_t x[5], all;
+        scan_bins(sh, x, all);
+        const uint32_t k = min((uint32_t)s.K, all);  // (fewer finite logits than K)
+        const int bin = bin_of(sh, x, k);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           if (4 * tid + i == bin) sh.out64[0] = x[i];
@@ -897,20 +909,24 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
 
   // the tile in which the running sum passes u * total, and the token
   __syncthreads();
-  double m0 = 0.0, m1 = 0.0, total;
+  u64 m0 = 0, m1 = 0, all;  // (integers: exactly one thread's two tiles hold the place)
   if (whole) {
-    if (2 * tid < a.ntile) m0 = sh.tmass[2 * tid];
-    if (2 * tid + 1 < a.ntile) m1 = sh.tmass[2 * tid + 1];
+    if (2 * tid < a.ntile) m0 = fixed44(sh.tmass[2 * tid]);
+    if (2 * tid + 1 < a.ntile) m1 = fixed44(sh.tmass[2 * tid + 1]);
   } else {
-    m0 = (double)sh.tsum[2 * tid] * 0x1p-44;
-    m1 = (double)sh.tsum[2 * tid + 1] * 0x1p-44;
+    m0 = sh.tsum[2 * tid];
+    m1 = sh.tsum[2 * tid + 1];
   }
-  const double base = wg_scan(m0 + m1, sh.red, total), t = (double)s.u * total;
-  int tile = wg_min(base + m0 > t && m0 > 0.0 ? 2 * tid : base + (m0 + m1) > t && m1 > 0.0 ? 2 * tid + 1 : INT_MAX, sh.red);
-  if (tile == INT_MAX)  // rounding: the last tile with any weight
-    tile = -wg_min(m1 > 0.0 ? -(2 * tid + 1) : m0 > 0.0 ? -2 * tid : INT_MAX, sh.red);
-  if (tid == tile / 2) sh.out64[0] = __double_as_longlong(base + (tile & 1 ? m0 : 0.0));
+  const u64 base = wg_scan(m0 + m1, sh.red, all);
+  const double total = (double)all * 0x1p-44, t = (double)s.u * total;
+  const u64 place = (u64)((double)s.u * (double)all);
+  if (base <= place && place < base + m0 + m1) {
+    const bool second = place >= base + m0;
+    sh.out32[0] = 2 * tid + second;
+    sh.out64[0] = base + (second ? m0 : 0);
+  }
   __syncthreads();
+  const int tile = sh.out32[0];
   if (wave == 0) {
     const f32x4 l = tile_quad(a, row, tile);
     const int j = tile * kTile + 4 * lane;
@@ -921,7 +937,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleK a) {
       if (!(w[e] >= mind)) w[e] = 0.0;
       ls += w[e];
     }
-    double run = __longlong_as_double(sh.out64[0]) + (wave_scan(ls) - ls);
+    double run = (double)sh.out64[0] * 0x1p-44 + (wave_scan(ls) - ls);
     int at = INT_MAX, last = -1;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
