@@ -17,10 +17,11 @@
 //                 above the bound in LDS, and keeps and draws there.  A row that is
 //                 not truncated is drawn from the tiles' sums and one tile.
 //                 A row that keeps more tokens than the list holds goes the long way:
-//                 a histogram of the row finds the last token kept, and a pass over it
-//                 sums what is kept.
+//                 a histogram of the row brackets the last token kept, and a pass over
+//                 it sums what lies above and lists the bracket.
 //   sample_probs  (rows x tile groups, if wanted) writes the distribution; tiles
 //                 without a kept token are written without being read.
+// A vocabulary of up to 64 tiles takes the three in one launch.
 // Bound by the one read of the logits (and the write of the distribution).
 #include <limits.h>
 

@@ -205,3 +205,13 @@ def test_broad_rows_of_large_batches(V, R, kw):
     for r in (0, 2, 3, 4, 9, 11, 33 % R):
         t1, p1, _ = _run(l[r:r + 1], u[r:r + 1], **kw)
         assert t1[0] == tok[r] and np.array_equal(p1[0], probs[r])
+
+
+@pytest.mark.parametrize("V", [4095, 4096, 4097, 16383, 16384, 16385])
+@pytest.mark.parametrize("kw", [dict(), dict(T=0.0), dict(k=50), dict(k=3000, p=0.9), dict(p=0.9), dict(p=0.99, T=3.0), dict(m=0.01), dict(k=200, m=0.05)])
+def test_vocabularies_about_the_small_ones(V, kw):
+    rng = np.random.default_rng(V)
+    l = (2 * rng.standard_normal((3, V))).astype(np.float32)
+    l[0, : V - 40] = -np.inf
+    l[1, -1] = 12.0
+    _check(l, rng.random(3).astype(np.float32), pad=V % 3, **kw)
