@@ -29,8 +29,11 @@ __device__ __forceinline__ double2 rope_angle(int pos, double inv_freq) {
 
 // grid (chunk_units, head groups of kStoreHeads): one page block of one
 // sequence, some heads.  16 lanes hold a (token, head) row, lane l the rotation
-// pairs (4l + e, 64 + 4l + e).
-constexpr int kStoreHeads = 8;
+// pairs (4l + e, 64 + 4l + e).  Bound by memory: a prompt of 8000 (8B layout, e4m3) with
+// its read back 77 us, 4.3 TB/s (81 with 8 heads a workgroup, 83 with 2, whose angles are
+// computed as often as they are used); 20 chunks of 100: 24.6, 26.7 and 25.8; 64 single
+// tokens, bound by their two launches: 9.7, 9.4 and 11.5.
+constexpr int kStoreHeads = 4;
 template <int PT>
 __global__ __launch_bounds__(256) void chunk_store_kernel(ChunkK a, const float* __restrict__ qkv, int64_t stride, int H,
                                                           int Hkv, RopeFreq64 f, bf16_t* __restrict__ q_out,

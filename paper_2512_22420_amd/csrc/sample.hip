@@ -22,7 +22,11 @@
 //   sample_probs  (rows x tile groups, if wanted) writes the distribution; tiles
 //                 without a kept token are written without being read.
 // A vocabulary of up to 64 tiles takes the three in one launch.
-// Bound by the one read of the logits (and the write of the distribution).
+// Bound by the one read of the logits (and the write of the distribution) in large
+// batches: 256 untruncated rows of 152064 57 us, 2.7 TB/s, 61 rows of 128256 by top-p with
+// the distribution 32 us; by the chain of a row's dependent steps in small ones: one row by
+// top-k and top-p 14 us; by a long row's two passes where there is one: 100 flat rows of
+// 152064 by top-p 123 us.
 #include <limits.h>
 
 #include "../../include/nightjar_serve.h"
